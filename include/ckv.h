@@ -300,6 +300,98 @@ int ckv_paged_compress(void* K_pool, void* V_pool, int32_t* deg_pool, int32_t* b
                        const ckv_paged_layout* pl, int32_t seq, const int32_t* seq_lens, const ckv_params* p,
                        int32_t* freed, int32_t freed_stride, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- block tables and slot maps, built on the GPU ---------------------------------------------
+ * A free list holds the blocks of a pool that belong to no sequence: device int32 [4 + 2 * n_blocks],
+ *   word 0       c, the number of free blocks;  words 1..3: zero (the calls use word 1 and leave it zero)
+ *   [4, 4 + c)   the free blocks, a stack: the last one is dealt first
+ *   [4 + n_blocks, 4 + 2 * n_blocks)   a mark per block, -1 = free, INT32_MAX = dealt.
+ * A new one holds c = n_blocks, the blocks n_blocks-1 ... 0 and marks of -1.  One free list serves the
+ * tables of all layers and sequences that share block numbers; a block belongs to one table row.  Calls
+ * on the same free list must not overlap in time.  Requests, lengths and counts stay on the device:
+ * nothing here synchronises, so every call can be recorded into a graph. */
+
+/* Blocks and slots for the next tokens of every sequence: sequence b goes from lens[b] to lens[b] + n_new[b]
+ * tokens (n_new[b] <= 0: none).  Requests are served in order, and one that does not fit is refused and left
+ * as it is: where its length is negative or the new one exceeds max_blocks * block_size; where the new tokens
+ * of the requests up to it exceed n_slots; where the blocks that the fitting requests up to it need exceed
+ * those that are free (a refused request's blocks count, so that later ones do not overtake it; one that
+ * needs no block is served).
+ *   block_table [batch, max_blocks], lens [batch]: updated for the requests that are served.
+ *   slots    int32 [n_slots]: the slot map: new token i of the packed order (sequence after sequence, refused
+ *            ones too) belongs in slot block * block_size + offset of the pool; -1 for tokens of refused
+ *            requests, for tokens whose table entry lies outside the pool and behind the last token.
+ *   starts   int32 [batch + 1] or NULL: first packed token of every sequence, then their number (no entry
+ *            exceeds n_slots).
+ *   granted  int32 [batch] or NULL: 1 where the request was served, 0 where it was refused.
+ * batch <= 4096; n_slots 0..2^30 (slots may be NULL when it is 0). */
+int ckv_paged_reserve(int32_t* block_table, int32_t* lens, const int32_t* n_new, int32_t* free_list, int32_t batch,
+                      int32_t max_blocks, int32_t n_blocks, int32_t block_size, int32_t* slots, int32_t n_slots,
+                      int32_t* starts, int32_t* granted, void* hip_stream);
+
+/* Shorten sequences: where 0 <= new_lens[b] < lens[b], the table entries behind the new length return to the
+ * free list and become -1, and lens[b] := new_lens[b]; other sequences are left as they are.  Entry order
+ * (row after row) is the order in which the blocks would be dealt again: trimming back what a reservation
+ * added leaves the free list as it was before.  Entries outside the pool and blocks that are free already
+ * are passed over; a block that several entries name returns once.  batch <= 4096, batch * max_blocks <= 2^30. */
+int ckv_paged_trim(int32_t* block_table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int32_t batch,
+                   int32_t max_blocks, int32_t n_blocks, int32_t block_size, void* hip_stream);
+
+/* Blocks ids[0..n) (device; what ckv_paged_compress and ckv_paged_scatter put into `freed`) return to the free
+ * list, with the same rules; the first of them would be dealt again first.  n <= 2^30. */
+int ckv_paged_free(const int32_t* ids, int32_t n, int32_t* free_list, int32_t n_blocks, void* hip_stream);
+
+/* Ragged rows into the cache: row i of k and v (its heads head_stride elements apart, rows row_stride elements
+ * apart, dim contiguous: a slice of a fused projection's output will do) goes to slot slots[i] of the pools,
+ * with degree 1 (deg_pool may be NULL).  Rows whose slot lies outside the pool are skipped; two rows with the
+ * same slot leave either of them, piece by piece.  Only heads, dim, dtype, block_size and n_blocks of the
+ * layout are looked at (the others have to be positive). */
+int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int32_t n,
+                    void* K_pool, void* V_pool, int32_t* deg_pool, const ckv_paged_layout* pl, void* hip_stream);
+
+/* ---- sparse decode attention over pages --------------------------------------------------------
+ * A decode step that reads the n_select most promising blocks per (sequence, KV head) instead of all.
+ *   bounds [n_blocks, heads, 2, dim] in the cache's dtype: per channel the least and the largest key of the
+ *          block's tokens;  mass int32 [n_blocks, heads]: the sum of their degrees.
+ * Supported by these three: bf16 dim 64/128; fp32 dim 32/64/128; pools of fewer than 2^31 token rows. */
+
+/* Bounds and mass of the blocks that hold tokens [since[b], min(lens[b], since[b] + max_new)) of every sequence,
+ * over all tokens of those blocks below lens[b] whose degree is above zero (deg_pool NULL: all, degree 1).
+ * since NULL = from the first token.  A channel with a NaN key has NaN bounds; a block without a token that counts
+ * has bounds (inf, -inf) and mass 0.  Call it with since = the lengths before whenever tokens were written (a
+ * block that is always read anyway, see n_recent, may wait), and for whole sequences after ckv_paged_compress
+ * or ckv_paged_scatter. */
+int ckv_paged_bounds(const void* K_pool, const int32_t* deg_pool, const int32_t* block_table, const int32_t* lens,
+                     const int32_t* since, const ckv_paged_layout* pl, int32_t max_new, void* bounds, int32_t* mass,
+                     void* hip_stream);
+
+/* The blocks to read.  Score of a block: ln(mass) + scale * max over the query heads of the KV head of
+ * sum_d max(q_d lo_d, q_d hi_d), an upper bound of the logarithm of the softmax mass that Eq. 3 gives the block's
+ * tokens; summed in 64 bits and rounded once to fp32, so that the selection does not hang on the order of sums.
+ * The first n_sink and the last n_recent blocks of a sequence are always taken, then those whose bounds, mass or
+ * query make no finite fp32 score, then the largest scores, ties to the lower block; blocks of mass <= 0 and table
+ * entries outside the pool come last.
+ *   lens [batch], max_len: as for ckv_paged_decode_attn.  n_sink + n_recent <= n_select.  scale <= 0 selects 1/sqrt(dim).
+ *   sel int32 [batch, heads, n_select]: block * heads + head for the selected blocks in ascending order of
+ *       position (-1 for one whose entry lies outside the pool), then -1.
+ *   sel_lens int32 [batch, heads]: tokens in them.
+ *   workspace: as for ckv_decode_attn, an int32 arrival counter per (sequence, KV head) comes first: zero-fill it
+ *       once when it is allocated; every call leaves the counters zero.  The size for a max_len serves every smaller
+ *       one; before a call with a larger batch * heads than it has served since, zero it again. */
+int ckv_paged_select_workspace(const ckv_paged_layout* pl, int32_t max_len, size_t* bytes);
+int ckv_paged_select(const void* q, int32_t q_heads, const void* bounds, const int32_t* mass, const int32_t* block_table,
+                     const int32_t* lens, const ckv_paged_layout* pl, int32_t max_len, int32_t n_select, int32_t n_sink,
+                     int32_t n_recent, float scale, int32_t* sel, int32_t* sel_lens, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
+
+/* ckv_paged_decode_attn over the selected blocks (Eq. 3 over their tokens).  sel, sel_lens: what ckv_paged_select
+ * wrote (a selection serves every layer whose pools share its block table).  Of the layout's max_blocks nothing is
+ * used.  Workspace contract and groupings as for ckv_decode_attn, with batch * heads counters; batch * heads <= 65535. */
+int ckv_paged_sparse_decode_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n_select, size_t* bytes);
+int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_pool, const void* V_pool,
+                                 const int32_t* deg_pool, const int32_t* sel, const int32_t* sel_lens,
+                                 const ckv_paged_layout* pl, int32_t n_select, float scale, void* o, int32_t o_dtype,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Per-kernel timing for benchmarks.  When enabled, every kernel launch of the calling process
  * is bracketed by HIP events on its stream (a few microseconds per launch, on the host and on the
  * GPU: 32 attention layers lose about a quarter of their speed to it).  ckv_timing_select narrows

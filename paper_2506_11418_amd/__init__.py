@@ -78,6 +78,8 @@ def _binding():
         L = lib()
         m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ckv_compress, L.ckv_append, L.ckv_decode_attn, L.ckv_paged_append,
                                                        L.ckv_paged_decode_attn)))
+        m.bind_tables(*(C.cast(f, C.c_void_p).value for f in (L.ckv_paged_reserve, L.ckv_paged_trim, L.ckv_paged_write, L.ckv_paged_bounds,
+                                                              L.ckv_paged_select, L.ckv_paged_sparse_decode_attn)))
         _native = m
     return _native
 
@@ -121,6 +123,16 @@ def lib() -> C.CDLL:
                                               C.POINTER(i32), C.POINTER(C.c_size_t)]
         L.ckv_paged_compress.argtypes = [vp, vp, vp, vp, vp, PL, i32, C.POINTER(i32), C.POINTER(Params), vp, i32, vp,
                                          C.c_size_t, vp]
+        sz = C.POINTER(C.c_size_t)
+        L.ckv_paged_reserve.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, vp]
+        L.ckv_paged_trim.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
+        L.ckv_paged_free.argtypes = [vp, i32, vp, i32, vp]
+        L.ckv_paged_write.argtypes = [vp, vp, C.c_int64, C.c_int64, vp, i32, vp, vp, vp, PL, vp]
+        L.ckv_paged_bounds.argtypes = [vp, vp, vp, vp, vp, PL, i32, vp, vp, vp]
+        L.ckv_paged_select_workspace.argtypes = [PL, i32, sz]
+        L.ckv_paged_select.argtypes = [vp, i32, vp, vp, vp, vp, PL, i32, i32, i32, i32, C.c_float, vp, vp, vp, C.c_size_t, vp]
+        L.ckv_paged_sparse_decode_attn_workspace.argtypes = [PL, i32, i32, sz]
+        L.ckv_paged_sparse_decode_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, PL, i32, C.c_float, vp, i32, vp, C.c_size_t, vp]
         L.ckv_bench_mfma_ceiling.argtypes = [i32, i32, i32, vp, C.c_size_t, C.POINTER(C.c_double), vp]
         L.ckv_timing_enable.argtypes = [C.c_int]
         L.ckv_timing_select.argtypes = [C.c_char_p]
@@ -199,6 +211,12 @@ def _stream():
 def _raw_stream() -> int:
     """The same as a number, without a Stream object.  (Only with a GPU tensor at hand.)"""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _here():
+    """The current GPU's number and its stream's.  (Only with a GPU tensor at hand.)"""
+    dev = torch._C._cuda_getDevice()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
 def match(K: torch.Tensor, chunk: int):
@@ -483,6 +501,264 @@ def paged_compress(K_pool, V_pool, deg_pool, block_table, seq: int, chunk: int, 
     if st != 0:
         raise CkvError(st, "ckv_paged_compress")
     return out_seq, freed
+
+
+# ---- block tables and slot maps, built on the GPU ----------------------------------------------
+def paged_free_list(n_blocks: int, device="cuda") -> torch.Tensor:
+    """A new free list: every block of a pool of n_blocks is free, block 0 is dealt first (int32 [4 + 2 * n_blocks], see
+    include/ckv.h for what it holds)."""
+    if n_blocks <= 0:
+        raise ValueError("a pool has at least one block")
+    t = torch.full((4 + 2 * n_blocks,), -1, dtype=torch.int32, device=device)
+    t[:4] = 0
+    t[0] = n_blocks
+    t[4:4 + n_blocks] = torch.arange(n_blocks - 1, -1, -1, dtype=torch.int32, device=device)
+    return t
+
+
+def _on_this_gpu(*tensors) -> None:
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.get_device() == here):
+            raise ValueError("all tensors must live on the current GPU")
+
+
+def _ints(what: str, t: torch.Tensor, *shape) -> None:
+    """An int32 tensor of this shape (None: any size), contiguous."""
+    if t.dtype != torch.int32 or t.dim() != len(shape) or not t.is_contiguous() or any(
+            n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what} must be a contiguous int32 [{', '.join('any' if n is None else str(n) for n in shape)}] tensor")
+
+
+def _pool_blocks(free_list: torch.Tensor) -> int:
+    _ints("free_list", free_list, None)
+    if free_list.numel() < 6 or free_list.numel() % 2:
+        raise ValueError("free_list must have 4 + 2 * n_blocks entries")
+    return (free_list.numel() - 4) // 2
+
+
+def paged_reserve(block_table, lens, n_new, free_list, block_size: int, n_slots: int, out: Optional[tuple] = None):
+    """ckv_paged_reserve: blocks and slots for n_new[b] more tokens of every sequence, on the GPU.  Updates block_table, lens and
+    free_list and returns (slots [n_slots], starts [batch + 1], granted [batch]); n_slots: the new tokens of all requests,
+    or more.  `out` may pass preallocated (slots, starts, granted)."""
+    if out is not None and block_table.is_cuda:
+        st = (_native or _binding()).paged_reserve(block_table, lens, n_new, free_list, block_size, n_slots, *out, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_reserve")
+    _ints("block_table", block_table, None, None)
+    B, width = block_table.shape
+    n_blocks = _pool_blocks(free_list)
+    _ints("lens", lens, B)
+    _ints("n_new", n_new, B)
+    if n_slots < 0:
+        raise ValueError("n_slots must not be negative")
+    if out is None:
+        out = tuple(torch.empty(n, dtype=torch.int32, device=block_table.device) for n in (n_slots, B + 1, B))
+    slots, starts, granted = out
+    _ints("slots", slots, n_slots)
+    _ints("starts", starts, B + 1)
+    _ints("granted", granted, B)
+    _on_this_gpu(block_table, lens, n_new, free_list, slots, starts, granted)
+    st = lib().ckv_paged_reserve(_ptr(block_table), _ptr(lens), _ptr(n_new), _ptr(free_list), B, width, n_blocks, block_size,
+                                 _ptr(slots), n_slots, _ptr(starts), _ptr(granted), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_reserve")
+    return slots, starts, granted
+
+
+def paged_trim(block_table, lens, new_lens, free_list, block_size: int) -> None:
+    """ckv_paged_trim: shorten sequences to new_lens[b] tokens where that is less than lens[b] and not negative; the blocks behind
+    return to the free list (0: a finished sequence gives back all of its blocks)."""
+    if block_table.is_cuda:
+        st = (_native or _binding()).paged_trim(block_table, lens, new_lens, free_list, block_size, *_here())
+        if st == 0:
+            return
+        if st is not None:
+            raise CkvError(st, "ckv_paged_trim")
+    _ints("block_table", block_table, None, None)
+    B, width = block_table.shape
+    n_blocks = _pool_blocks(free_list)
+    _ints("lens", lens, B)
+    _ints("new_lens", new_lens, B)
+    _on_this_gpu(block_table, lens, new_lens, free_list)
+    st = lib().ckv_paged_trim(_ptr(block_table), _ptr(lens), _ptr(new_lens), _ptr(free_list), B, width, n_blocks, block_size,
+                              _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_trim")
+
+
+def paged_free(ids, free_list) -> None:
+    """ckv_paged_free: blocks (any contiguous int32 tensor of their numbers, -1 = none: what paged_compress and paged_scatter
+    return) go back to the free list."""
+    n_blocks = _pool_blocks(free_list)
+    if ids.dtype != torch.int32 or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 tensor")
+    _on_this_gpu(ids, free_list)
+    st = lib().ckv_paged_free(_ptr(ids), ids.numel(), _ptr(free_list), n_blocks, _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_free")
+
+
+def paged_write(k, v, slots, K_pool, V_pool, deg_pool=None) -> None:
+    """ckv_paged_write: rows k, v [n, heads, dim] (dim contiguous, both with the same strides) into the pools at their slots, with
+    degree 1; rows of slot -1 are skipped."""
+    if K_pool.is_cuda:
+        st = (_native or _binding()).paged_write(k, v, slots, K_pool, V_pool, deg_pool, *_here())
+        if st == 0:
+            return
+        if st is not None:
+            raise CkvError(st, "ckv_paged_write")
+    nb, H, bs, D = _pools(K_pool, V_pool, deg_pool)
+    n = slots.numel()
+    _ints("slots", slots, n)
+    for t in (k, v):
+        if tuple(t.shape) != (n, H, D) or t.dtype != K_pool.dtype or t.stride(2) != 1:
+            raise ValueError("k, v must be [slots, heads, dim] tensors of the cache dtype with contiguous dim")
+    if k.stride() != v.stride():
+        raise ValueError("k and v must share strides")
+    _on_this_gpu(k, v, slots, K_pool, V_pool, deg_pool)
+    pl = PagedLayout(1, H, D, _DT[K_pool.dtype], bs, 1, nb)
+    row, head = (k.stride(0) if n > 1 else H * D), (k.stride(1) if H > 1 else D)
+    st = lib().ckv_paged_write(_ptr(k), _ptr(v), row, head, _ptr(slots), n, _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool), C.byref(pl),
+                               _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_write")
+
+
+def _pools(K_pool, V_pool, deg_pool):
+    """The shape of a pool and what belongs to it, checked."""
+    for t in (K_pool, V_pool):
+        if t.dim() != 4 or not t.is_contiguous() or t.dtype not in _DT or t.shape != K_pool.shape or t.dtype != K_pool.dtype:
+            raise ValueError("pools must be contiguous [n_blocks, heads, block_size, dim] float32/bfloat16 tensors of one shape")
+    if deg_pool is not None:
+        _ints("deg_pool", deg_pool, *K_pool.shape[:3])
+    return K_pool.shape
+
+
+# ---- sparse decode attention over pages --------------------------------------------------------
+def paged_bounds(K_pool, deg_pool, block_table, lens, max_new: int, since=None, out: Optional[tuple] = None):
+    """ckv_paged_bounds: (bounds [n_blocks, heads, 2, dim], mass int32 [n_blocks, heads]) of the blocks that hold tokens
+    [since[b], min(lens[b], since[b] + max_new)); since None: from the first.  `out` passes the tensors to update; without it they
+    are made new, zero for blocks of other tokens."""
+    if out is not None and K_pool.is_cuda:
+        st = (_native or _binding()).paged_bounds(K_pool, deg_pool, block_table, lens, since, max_new, *out, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_bounds")
+    pl = paged_layout_of(K_pool, block_table)
+    nb, H, _, D = _pools(K_pool, K_pool, deg_pool)
+    _ints("lens", lens, pl.batch)
+    if since is not None:
+        _ints("since", since, pl.batch)
+    if out is None:
+        out = (torch.zeros((nb, H, 2, D), dtype=K_pool.dtype, device=K_pool.device),
+               torch.zeros((nb, H), dtype=torch.int32, device=K_pool.device))
+    bounds, mass = out
+    _bounds_of(bounds, mass, nb, H, D, K_pool.dtype)
+    _on_this_gpu(K_pool, deg_pool, block_table, lens, since, bounds, mass)
+    st = lib().ckv_paged_bounds(_ptr(K_pool), _ptr(deg_pool), _ptr(block_table), _ptr(lens), _ptr(since), C.byref(pl), max_new,
+                                _ptr(bounds), _ptr(mass), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_bounds")
+    return bounds, mass
+
+
+def _bounds_of(bounds, mass, nb, H, D, dtype) -> None:
+    if tuple(bounds.shape) != (nb, H, 2, D) or bounds.dtype != dtype or not bounds.is_contiguous():
+        raise ValueError("bounds must be a contiguous [n_blocks, heads, 2, dim] tensor of the cache dtype")
+    _ints("mass", mass, nb, H)
+
+
+def paged_select_workspace(pl: PagedLayout, max_len: int) -> int:
+    n = C.c_size_t(0)
+    st = lib().ckv_paged_select_workspace(C.byref(pl), max_len, C.byref(n))
+    if st != 0:
+        raise CkvError(st, "ckv_paged_select_workspace")
+    return n.value
+
+
+def paged_select(q, bounds, mass, block_table, lens, max_len: int, n_select: int, block_size: int, n_sink: int = 1,
+                 n_recent: int = 1, scale: float = 0.0, out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None):
+    """ckv_paged_select: the n_select blocks per (sequence, KV head) with the largest upper bound of softmax mass for q
+    [batch, q_heads, dim], the first n_sink and last n_recent always among them: (sel [batch, heads, n_select], sel_lens
+    [batch, heads]) for paged_sparse_decode_attn.  `out` may pass both; a `workspace` passed in must have been zero-filled when
+    it was allocated."""
+    if out is not None and workspace is not None and q.is_cuda:
+        st = (_native or _binding()).paged_select(q, bounds, mass, block_table, lens, max_len, n_select, block_size, n_sink, n_recent,
+                                                  scale, *out, workspace, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_select")
+    if q.dim() != 3 or not q.is_contiguous() or q.dtype not in _DT:
+        raise ValueError("q must be a contiguous [batch, q_heads, dim] float32/bfloat16 tensor")
+    _ints("block_table", block_table, q.shape[0], None)
+    _ints("lens", lens, q.shape[0])
+    if mass.dim() != 2:
+        raise ValueError("mass must be a contiguous int32 [n_blocks, heads] tensor")
+    (nb, H), (B, q_heads, D) = mass.shape, q.shape
+    _bounds_of(bounds, mass, nb, H, D, q.dtype)
+    pl = PagedLayout(B, H, D, _DT[q.dtype], block_size, block_table.shape[1], nb)
+    if n_select <= 0:
+        raise ValueError("n_select must be positive")
+    if out is None:
+        out = (torch.empty((B, H, n_select), dtype=torch.int32, device=q.device), torch.empty((B, H), dtype=torch.int32, device=q.device))
+    sel, sel_lens = out
+    _ints("sel", sel, B, H, n_select)
+    _ints("sel_lens", sel_lens, B, H)
+    if workspace is None:
+        workspace = torch.zeros(paged_select_workspace(pl, max_len), dtype=torch.uint8, device=q.device)
+    _on_this_gpu(q, bounds, mass, block_table, lens, sel, sel_lens, workspace)
+    st = lib().ckv_paged_select(_ptr(q), q_heads, _ptr(bounds), _ptr(mass), _ptr(block_table), _ptr(lens), C.byref(pl), max_len,
+                                n_select, n_sink, n_recent, scale, _ptr(sel), _ptr(sel_lens), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_select")
+    return sel, sel_lens
+
+
+def paged_sparse_decode_attn_workspace(pl: PagedLayout, q_heads: int, n_select: int) -> int:
+    n = C.c_size_t(0)
+    st = lib().ckv_paged_sparse_decode_attn_workspace(C.byref(pl), q_heads, n_select, C.byref(n))
+    if st != 0:
+        raise CkvError(st, "ckv_paged_sparse_decode_attn_workspace")
+    return n.value
+
+
+def paged_sparse_decode_attn(q, K_pool, V_pool, deg_pool, sel, sel_lens, scale: float = 0.0, out_dtype=None, out=None,
+                             workspace=None):
+    """ckv_paged_sparse_decode_attn: Eq. 3 over the blocks that paged_select chose.  q [batch, q_heads, dim] -> o of its shape.
+    A `workspace` passed in must have been zero-filled when it was allocated."""
+    if out is not None and workspace is not None and q.is_cuda:
+        st = (_native or _binding()).paged_sparse_decode_attn(q, K_pool, V_pool, deg_pool, sel, sel_lens, scale, out, workspace, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_sparse_decode_attn")
+    nb, H, bs, D = _pools(K_pool, V_pool, deg_pool)
+    if q.dim() != 3 or not q.is_contiguous() or q.dtype != K_pool.dtype or q.shape[2] != D:
+        raise ValueError("q must be a contiguous [batch, q_heads, dim] tensor of the cache dtype")
+    B, q_heads = q.shape[:2]
+    _ints("sel", sel, B, H, None)
+    _ints("sel_lens", sel_lens, B, H)
+    n_select = sel.shape[2]
+    pl = PagedLayout(B, H, D, _DT[K_pool.dtype], bs, max(n_select, 1), nb)
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    if out.shape != q.shape or not out.is_contiguous() or out.dtype not in _DT:
+        raise ValueError("out must be a contiguous float32/bfloat16 tensor of the query's shape")
+    if workspace is None:
+        workspace = torch.zeros(paged_sparse_decode_attn_workspace(pl, q_heads, n_select), dtype=torch.uint8, device=q.device)
+    _on_this_gpu(q, K_pool, V_pool, deg_pool, sel, sel_lens, out, workspace)
+    st = lib().ckv_paged_sparse_decode_attn(_ptr(q), q_heads, _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool), _ptr(sel), _ptr(sel_lens),
+                                            C.byref(pl), n_select, scale, _ptr(out), _DT[out.dtype], _ptr(workspace),
+                                            workspace.numel() * workspace.element_size(), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_sparse_decode_attn")
+    return out
 
 
 def mfma_ceiling(mode: int, waves_per_cu: int, iters: int = 20000) -> float:

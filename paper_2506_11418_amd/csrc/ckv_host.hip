@@ -3,6 +3,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -852,6 +853,207 @@ int ckv_paged_compress(void* K_pool, void* V_pool, int32_t* deg_pool, int32_t* b
     if (err != hipSuccess) return ckv::hip_status(err);
   }
   return CKV_OK;
+}
+
+// ---- block tables and slot maps ------------------------------------------------------------------
+namespace {
+constexpr int32_t kMostEntries = 1 << 30;   // slots, ids or table entries of one call: indexed in 32 bits
+int check_tables(int32_t batch, int32_t max_blocks, int32_t n_blocks, int32_t block_size, int* shift) {
+  ckv_paged_layout pl{batch, 1, 4, CKV_F32, block_size, max_blocks, n_blocks};
+  const int st = check_paged(&pl, shift);
+  if (st != CKV_OK) return st;
+  if (batch > 4096) return CKV_ESHAPE;
+  if ((int64_t)batch * max_blocks > kMostEntries) return CKV_ESHAPE;
+  if ((int64_t)n_blocks * block_size > INT32_MAX || n_blocks > kMostEntries) return CKV_EUNSUPPORTED;   // slots are 32 bits
+  return CKV_OK;
+}
+// whether no two of these overlap (NULL and empty ones do not)
+struct Span { const void* p; size_t bytes; };
+bool apart(std::initializer_list<Span> all) {
+  for (const Span& a : all)
+    for (const Span& b : all)
+      if (&a != &b && a.p && b.p && a.bytes && b.bytes && ckv::overlaps(a.p, a.bytes, b.p, b.bytes)) return false;
+  return true;
+}
+bool misaligned4(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if ((uintptr_t)p % 4) return true;
+  return false;
+}
+}  // namespace
+
+int ckv_paged_reserve(int32_t* block_table, int32_t* lens, const int32_t* n_new, int32_t* free_list, int32_t batch,
+                      int32_t max_blocks, int32_t n_blocks, int32_t block_size, int32_t* slots, int32_t n_slots,
+                      int32_t* starts, int32_t* granted, void* hip_stream) {
+  int shift;
+  int st = check_tables(batch, max_blocks, n_blocks, block_size, &shift);
+  if (st != CKV_OK) return st;
+  if (n_slots < 0 || n_slots > kMostEntries) return CKV_ESHAPE;
+  if (!block_table || !lens || !n_new || !free_list || (!slots && n_slots > 0)) return CKV_EINVAL;
+  if (misaligned4({block_table, lens, n_new, free_list, slots, starts, granted})) return CKV_EALIGN;
+  const size_t n = (size_t)batch * 4, table = n * max_blocks, list = 16 + (size_t)n_blocks * 8;
+  if (!apart({{block_table, table}, {lens, n}, {n_new, n}, {free_list, list}, {slots, (size_t)n_slots * 4}, {starts, n + 4}, {granted, n}}))
+    return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_reserve(block_table, lens, n_new, free_list, batch, max_blocks, n_blocks, shift, slots,
+                                                   n_slots, starts, granted, static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_trim(int32_t* block_table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int32_t batch,
+                   int32_t max_blocks, int32_t n_blocks, int32_t block_size, void* hip_stream) {
+  int shift;
+  int st = check_tables(batch, max_blocks, n_blocks, block_size, &shift);
+  if (st != CKV_OK) return st;
+  if (!block_table || !lens || !new_lens || !free_list) return CKV_EINVAL;
+  if (misaligned4({block_table, lens, new_lens, free_list})) return CKV_EALIGN;
+  const size_t n = (size_t)batch * 4;
+  if (!apart({{block_table, n * max_blocks}, {lens, n}, {new_lens, n}, {free_list, 16 + (size_t)n_blocks * 8}})) return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_trim(block_table, lens, new_lens, free_list, batch, max_blocks, n_blocks, shift,
+                                                static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_free(const int32_t* ids, int32_t n, int32_t* free_list, int32_t n_blocks, void* hip_stream) {
+  if (n < 0 || n > kMostEntries || n_blocks <= 0) return CKV_ESHAPE;
+  if (n_blocks > kMostEntries) return CKV_EUNSUPPORTED;
+  if ((!ids && n > 0) || !free_list) return CKV_EINVAL;
+  if (misaligned4({ids, free_list})) return CKV_EALIGN;
+  if (!apart({{ids, (size_t)n * 4}, {free_list, 16 + (size_t)n_blocks * 8}})) return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_free(ids, n, free_list, n_blocks, static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int32_t n,
+                    void* K_pool, void* V_pool, int32_t* deg_pool, const ckv_paged_layout* pl, void* hip_stream) {
+  int shift;
+  int st = check_paged(pl, &shift);
+  if (st != CKV_OK) return st;
+  const int e = ckv::elem_bytes(pl->dtype);
+  if (n < 0 || n > kMostEntries || (int64_t)pl->heads * pl->dim * e > INT32_MAX) return CKV_ESHAPE;
+  if ((int64_t)pl->n_blocks * pl->block_size > INT32_MAX) return CKV_EUNSUPPORTED;   // slots are 32 bits
+  if (n == 0) return CKV_OK;
+  if (!k || !v || !slots || !K_pool || !V_pool) return CKV_EINVAL;
+  if (head_stride < pl->dim || row_stride < pl->dim) return CKV_ESHAPE;
+  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)K_pool | (uintptr_t)V_pool) % 16 || row_stride * e % 16 || head_stride * e % 16)
+    return CKV_EALIGN;
+  if (misaligned4({slots, deg_pool})) return CKV_EALIGN;
+  const size_t in = (size_t)((int64_t)(n - 1) * row_stride + (int64_t)(pl->heads - 1) * head_stride + pl->dim) * e;   // (k and v may share rows)
+  const size_t pool = (size_t)pl->n_blocks * pl->heads * pl->block_size * pl->dim * e;
+  if (!apart({{k, in}, {K_pool, pool}, {V_pool, pool}}) || !apart({{v, in}, {K_pool, pool}, {V_pool, pool}})) return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_write(k, v, row_stride * e, head_stride * e, slots, n, K_pool, V_pool, deg_pool, pl->heads,
+                                                 pl->dim * e, shift, pl->n_blocks, static_cast<hipStream_t>(hip_stream)));
+}
+
+// ---- sparse decode attention over pages ----------------------------------------------------------
+namespace {
+int check_sparse(const ckv_paged_layout* pl, int* shift) {
+  const int st = check_paged(pl, shift);
+  if (st != CKV_OK) return st;
+  if ((int64_t)pl->n_blocks * pl->heads * pl->block_size > INT32_MAX) return CKV_EUNSUPPORTED;   // pool rows are indexed in 32 bits
+  if (pl->dtype == CKV_BF16 ? !(pl->dim == 64 || pl->dim == 128) : !(pl->dim == 32 || pl->dim == 64 || pl->dim == 128))
+    return CKV_EUNSUPPORTED;
+  if (pl->batch > 65535 || pl->heads > 65535) return CKV_EUNSUPPORTED;   // (dimensions of a launch)
+  return CKV_OK;
+}
+int key_stride(const ckv_paged_layout* pl, int32_t max_len) {
+  const int64_t n = ((int64_t)max_len + pl->block_size - 1) / pl->block_size;
+  return (int)(n < pl->max_blocks ? n : pl->max_blocks);
+}
+// the layout of the selected blocks: every (sequence, KV head) a sequence of one head, every (block, head) a block
+int sparse_layout(const ckv_paged_layout* pl, int32_t n_select, ckv_paged_layout* out) {
+  if (n_select <= 0 || (int64_t)n_select * pl->block_size > INT32_MAX) return CKV_ESHAPE;
+  if ((int64_t)pl->batch * pl->heads > 65535) return CKV_EUNSUPPORTED;   // (a dimension of the launch)
+  *out = *pl;
+  out->batch = pl->batch * pl->heads;
+  out->heads = 1;
+  out->n_blocks = pl->n_blocks * pl->heads;
+  out->max_blocks = n_select;
+  return CKV_OK;
+}
+}  // namespace
+
+int ckv_paged_bounds(const void* K_pool, const int32_t* deg_pool, const int32_t* block_table, const int32_t* lens,
+                     const int32_t* since, const ckv_paged_layout* pl, int32_t max_new, void* bounds, int32_t* mass,
+                     void* hip_stream) {
+  int shift;
+  int st = check_sparse(pl, &shift);
+  if (st != CKV_OK) return st;
+  if (max_new <= 0) return CKV_ESHAPE;
+  if (!K_pool || !block_table || !lens || !bounds || !mass) return CKV_EINVAL;
+  if (((uintptr_t)K_pool | (uintptr_t)bounds) % 16 || misaligned4({deg_pool, block_table, lens, since, mass})) return CKV_EALIGN;
+  const size_t e = ckv::elem_bytes(pl->dtype), pairs = (size_t)pl->n_blocks * pl->heads;
+  if (ckv::overlaps(K_pool, pairs * pl->block_size * pl->dim * e, bounds, pairs * 2 * pl->dim * e)) return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_bounds(K_pool, deg_pool, pl->dtype, ckv::PagedView{block_table, pl->max_blocks, shift, pl->n_blocks},
+                                                  lens, since, max_new, pl->batch, pl->heads, pl->dim, bounds, mass,
+                                                  static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_select_workspace(const ckv_paged_layout* pl, int32_t max_len, size_t* bytes) {
+  int shift;
+  int st = check_sparse(pl, &shift);
+  if (st != CKV_OK) return st;
+  if (!bytes) return CKV_EINVAL;
+  if (max_len <= 0) return CKV_ESHAPE;
+  const size_t rows = (size_t)pl->batch * pl->heads;
+  *bytes = ckv::align_up(ckv::attn_counter_bytes(pl->batch, pl->heads) + rows * key_stride(pl, max_len) * sizeof(uint32_t), 256);
+  return CKV_OK;
+}
+
+int ckv_paged_select(const void* q, int32_t q_heads, const void* bounds, const int32_t* mass, const int32_t* block_table,
+                     const int32_t* lens, const ckv_paged_layout* pl, int32_t max_len, int32_t n_select, int32_t n_sink,
+                     int32_t n_recent, float scale, int32_t* sel, int32_t* sel_lens, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+  size_t need = 0;
+  int st = ckv_paged_select_workspace(pl, max_len, &need);   // validates the layout and max_len
+  if (st != CKV_OK) return st;
+  if (q_heads <= 0 || q_heads % pl->heads) return CKV_ESHAPE;
+  if (n_select <= 0 || (int64_t)n_select * pl->block_size > INT32_MAX) return CKV_ESHAPE;
+  if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > n_select) return CKV_EINVAL;
+  if (!q || !bounds || !mass || !block_table || !lens || !sel || !sel_lens || !workspace) return CKV_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)bounds | (uintptr_t)workspace) % 16 || misaligned4({mass, block_table, lens, sel, sel_lens}))
+    return CKV_EALIGN;
+  if (workspace_bytes < need) return CKV_EWORKSPACE;
+  const int G = q_heads / pl->heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return CKV_EUNSUPPORTED;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)pl->dim);
+  int shift;
+  check_paged(pl, &shift);
+  const int64_t cap = (int64_t)pl->max_blocks * pl->block_size;
+  ckv::SelectCall c{};
+  c.q = q; c.bounds = bounds; c.mass = mass;
+  c.paged = ckv::PagedView{block_table, pl->max_blocks, shift, pl->n_blocks};
+  c.lens = lens;
+  c.max_len = (int)(max_len < cap ? max_len : cap);
+  c.n_b = pl->batch; c.heads = pl->heads; c.dim = pl->dim;
+  c.n_select = n_select; c.n_sink = n_sink; c.n_recent = n_recent;
+  c.scale = scale;
+  c.arrived = static_cast<int32_t*>(workspace);
+  c.keys = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + ckv::attn_counter_bytes(pl->batch, pl->heads));
+  c.key_stride = key_stride(pl, max_len);
+  c.sel = sel; c.sel_lens = sel_lens;
+  c.st = static_cast<hipStream_t>(hip_stream);
+  return ckv::hip_status(ckv::launch_paged_select(pl->dtype, G, c));
+}
+
+int ckv_paged_sparse_decode_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n_select, size_t* bytes) {
+  int shift;
+  int st = check_sparse(pl, &shift);
+  if (st != CKV_OK) return st;
+  if (q_heads <= 0 || q_heads % pl->heads) return CKV_ESHAPE;
+  ckv_paged_layout sl;
+  st = sparse_layout(pl, n_select, &sl);
+  if (st != CKV_OK) return st;
+  return ckv_paged_decode_attn_workspace(&sl, q_heads / pl->heads, n_select * pl->block_size, bytes);
+}
+
+int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_pool, const void* V_pool,
+                                 const int32_t* deg_pool, const int32_t* sel, const int32_t* sel_lens,
+                                 const ckv_paged_layout* pl, int32_t n_select, float scale, void* o, int32_t o_dtype,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream) {
+  size_t reserve = 0;
+  int st = ckv_paged_sparse_decode_attn_workspace(pl, q_heads, n_select, &reserve);   // validates the layout and the numbers
+  if (st != CKV_OK) return st;
+  ckv_paged_layout sl;
+  sparse_layout(pl, n_select, &sl);
+  return ckv_paged_decode_attn(q, q_heads / pl->heads, K_pool, V_pool, deg_pool, sel, sel_lens, &sl, n_select * pl->block_size, scale,
+                               o, o_dtype, workspace, workspace_bytes, hip_stream);
 }
 
 int ckv_timing_enable(int on) {

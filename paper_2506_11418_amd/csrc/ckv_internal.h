@@ -207,6 +207,36 @@ hipError_t launch_paged_scatter(const void* K, const void* V, const int32_t* deg
                                 int keep_blocks, int old_blocks, int32_t* freed, int freed_stride, int32_t* lens,
                                 hipStream_t st);
 
+// ---- tables, slots and sparse attention of paged caches -----------------------------------------
+// see k8_tables.hip; free_list: int32 [4 + 2 * n_blocks]
+hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_new, int32_t* free_list, int n_b, int max_blocks,
+                                int n_blocks, int shift, int32_t* slots, int n_slots, int32_t* starts, int32_t* granted,
+                                hipStream_t st);
+hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int n_b, int max_blocks,
+                             int n_blocks, int shift, hipStream_t st);
+hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int n_blocks, hipStream_t st);
+// strides in bytes
+hipError_t launch_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int n,
+                              void* K_pool, void* V_pool, int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
+                              hipStream_t st);
+// see k9_sparse.hip; tokens [since[b], min(lens[b], since[b] + max_new)) of every sequence, since NULL = from 0
+hipError_t launch_paged_bounds(const void* K, const int32_t* deg, int dtype, PagedView paged, const int32_t* lens, const int32_t* since,
+                               int max_new, int n_b, int heads, int dim, void* bounds, int32_t* mass, hipStream_t st);
+struct SelectCall {
+  const void *q, *bounds;
+  const int32_t* mass;
+  PagedView paged;
+  const int32_t* lens;
+  int max_len, n_b, heads, dim, n_select, n_sink, n_recent;
+  float scale;
+  int32_t* arrived;       // a counter a (sequence, head), zero between calls
+  uint32_t* keys;         // [n_b, heads, key_stride]: a rank a block
+  int key_stride;
+  int32_t *sel, *sel_lens;
+  hipStream_t st;
+};
+hipError_t launch_paged_select(int dtype, int G, const SelectCall& c);
+
 // ---- timing hooks ----------------------------------------------------------------------------
 // One-time set-up of a kernel that needs more than the default dynamic LDS, per device (each device
 // holds its own copy of the code object, so the limit is raised on each one that launches it).

@@ -1,0 +1,295 @@
+// Block tables and slot maps of a block-paged cache, built on the GPU: which blocks a step's new tokens go to, the blocks that
+// sequences give back, and the copy of ragged rows into their slots.
+//
+// Free list: int32 [4 + 2 n_blocks].  Word 0: the number c of free blocks, word 1: an arrival counter that is zero between
+// calls, words 2 and 3 unused; then the stack, whose first c entries are the free blocks, the next one to be dealt last; then one
+// mark a block, -1 for a free one and INT_MAX for one that is dealt (a block that is given back twice is taken once).
+#include "ckv_internal.h"
+#include "ckv_device.h"
+
+namespace ckv {
+namespace {
+
+constexpr int kListHead = 4;
+constexpr int kInUse = INT32_MAX;
+
+__device__ __forceinline__ int blocks_of(int tokens, int shift) { return (tokens >> shift) + ((tokens & ((1 << shift) - 1)) != 0); }
+
+// Sums over this thread and the threads before it, each cut to `most` (x is, and 2 * most fits 32 bits); `all` receives the
+// sum of the whole workgroup.  s_wave: one word a wave.
+template <int THREADS>
+__device__ __forceinline__ uint32_t scan_capped(uint32_t x, uint32_t most, uint32_t* s_wave, uint32_t& all) {
+  constexpr int W = THREADS / 64;
+#define CKV_SCAN_STEP(ctrl, rows) x = min(x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xF, false), most)
+  CKV_SCAN_STEP(0x111, 0xF);               // a row of 16: one, two, four, eight lanes up
+  CKV_SCAN_STEP(0x112, 0xF);
+  CKV_SCAN_STEP(0x114, 0xF);
+  CKV_SCAN_STEP(0x118, 0xF);
+  CKV_SCAN_STEP(0x142, 0xA);               // the last lane of rows 0 and 2 into rows 1 and 3
+  CKV_SCAN_STEP(0x143, 0xC);               // lane 31 into rows 2 and 3
+#undef CKV_SCAN_STEP
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 63) s_wave[wave] = x;
+  __syncthreads();
+  uint32_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    if (w == wave) before = all;
+    all = min(all + s_wave[w], most);
+  }
+  __syncthreads();                         // (s_wave is free again)
+  return min(x + before, most);
+}
+
+// first i in [0, n) with end[i] > x (end does not fall; there is one)
+__device__ __forceinline__ int owner_of(const int32_t* end, int n, int x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (end[mid] > x) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+constexpr int kReserveThreads = 256, kSlotsPerGroup = 1024;
+
+// Every workgroup works out for itself who gets what (two running sums over the requests, in LDS), then writes its share of
+// the slots and of the table entries: a request's j-th new token is token L + j of its row, in the entry the row has there
+// already or in one that this call deals, the i-th block dealt being the i-th from the stack's top.  Nothing that one workgroup
+// writes is read by another: lengths and the number of free blocks change when the last one has read them.
+// dynamic LDS: 12 bytes a request
+__global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
+    int32_t* __restrict__ table, int32_t* __restrict__ lens, const int32_t* __restrict__ n_new, int32_t* __restrict__ free_list,
+    int n_b, int max_blocks, int n_blocks, int shift, int32_t* __restrict__ slots, int n_slots, int32_t* __restrict__ starts,
+    int32_t* __restrict__ granted) {
+  extern __shared__ int32_t s_dyn[];
+  int32_t *s_end = s_dyn, *s_dealt = s_dyn + n_b, *s_len = s_dyn + 2 * n_b;   // sums up to each request; its length, -1: refused
+  __shared__ uint32_t s_wave[kReserveThreads / 64];
+  __shared__ int s_take, s_last;
+  const int tid = threadIdx.x;
+  const int n_free = min(max(free_list[0], 0), n_blocks);
+  const int32_t* stack = free_list + kListHead;
+  int32_t* marks = free_list + kListHead + n_blocks;
+  const int64_t row_tokens = (int64_t)max_blocks << shift;
+  const uint32_t most_tokens = (uint32_t)n_slots + 1, most_blocks = (uint32_t)n_blocks + 1;   // (more than there is: how much more does not matter)
+  uint32_t tokens = 0, blocks = 0;
+  if (tid == 0) s_take = 0;
+  for (int b0 = 0; b0 < n_b; b0 += kReserveThreads) {
+    const int b = b0 + tid;
+    int len = -1, n = 0;
+    if (b < n_b) { len = lens[b]; n = max(n_new[b], 0); }
+    uint32_t all;
+    const uint32_t end = min(scan_capped<kReserveThreads>(min((uint32_t)n, most_tokens), most_tokens, s_wave, all) + tokens, most_tokens);
+    tokens = min(tokens + all, most_tokens);
+    const bool fits = len >= 0 && (int64_t)len + n <= row_tokens && end <= (uint32_t)n_slots;
+    const int need = fits ? blocks_of(len + n, shift) - blocks_of(len, shift) : 0;
+    const uint32_t dealt = min(scan_capped<kReserveThreads>(min((uint32_t)need, most_blocks), most_blocks, s_wave, all) + blocks, most_blocks);
+    blocks = min(blocks + all, most_blocks);
+    const bool ok = fits && (need == 0 || dealt <= (uint32_t)n_free);
+    if (b < n_b) {
+      s_end[b] = (int)min(end, (uint32_t)n_slots);
+      s_dealt[b] = (int)dealt;
+      s_len[b] = ok ? len : -1;
+      if (ok && need > 0) atomicMax(&s_take, (int)dealt);
+    }
+  }
+  __syncthreads();
+  const int total = s_end[n_b - 1], take = s_take;
+  for (int j = blockIdx.x * kReserveThreads + tid; j < n_slots; j += gridDim.x * kReserveThreads) {
+    int slot = -1;
+    if (j < total) {
+      const int b = owner_of(s_end, n_b, j), len = s_len[b];
+      if (len >= 0) {
+        const int t = len + (j - (b ? s_end[b - 1] : 0)), have = blocks_of(len, shift);
+        const int at = t >> shift;
+        const int blk = at < have ? table[(int64_t)b * max_blocks + at]
+                                  : stack[max(n_free - 1 - ((b ? s_dealt[b - 1] : 0) + (at - have)), 0)];
+        if ((unsigned)blk < (unsigned)n_blocks) slot = (blk << shift) + (t & ((1 << shift) - 1));
+      }
+    }
+    slots[j] = slot;
+    if (j < take) {                        // (no request takes more blocks than tokens)
+      const int b = owner_of(s_dealt, n_b, j), k = j - (b ? s_dealt[b - 1] : 0);
+      const int blk = stack[n_free - 1 - j];
+      table[(int64_t)b * max_blocks + blocks_of(s_len[b], shift) + k] = blk;
+      if ((unsigned)blk < (unsigned)n_blocks) marks[blk] = kInUse;
+    }
+  }
+  if (blockIdx.x == 0) {
+    for (int b = tid; b < n_b; b += kReserveThreads) {
+      if (starts) starts[b + 1] = s_end[b];
+      if (granted) granted[b] = s_len[b] >= 0;
+    }
+    if (starts && tid == 0) starts[0] = 0;
+  }
+  if (gridDim.x > 1) {
+    __syncthreads();                       // (what this workgroup read has arrived: it has been stored or compared)
+    if (tid == 0) s_last = atomicAdd(&free_list[1], 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+  } else {
+    __syncthreads();
+  }
+  for (int b = tid; b < n_b; b += kReserveThreads)
+    if (s_len[b] >= 0) lens[b] = s_len[b] + max(n_new[b], 0);
+  if (tid == 0) {
+    free_list[0] = n_free - take;
+    if (gridDim.x > 1) atomicExch(&free_list[1], 0);
+  }
+}
+
+constexpr int kReturnThreads = 1024, kPerThread = 4;
+
+// Blocks back onto the stack, in one workgroup: the order on the stack is that of the entries, the last one first, so that a
+// reservation that is taken back leaves the stack as it was.  An entry outside the pool, or one whose block is free already,
+// is passed over; of several entries with the same block one is taken: each leaves its place in the block's mark, and the
+// least one stays.
+// TABLE: the entries of each row behind new_lens[b] tokens, which become -1; else the n_ids entries of `entries`.
+// dynamic LDS (TABLE): 4 bytes a row
+template <bool TABLE>
+__global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* __restrict__ entries, int n_ids, int max_blocks,
+                                                                      int n_b, int32_t* __restrict__ lens,
+                                                                      const int32_t* __restrict__ new_lens,
+                                                                      int32_t* __restrict__ free_list, int n_blocks, int shift) {
+  extern __shared__ int32_t s_end[];       // entries up to each row, the last row first
+  __shared__ uint32_t s_wave[kReturnThreads / 64];
+  const int tid = threadIdx.x;
+  int32_t* stack = free_list + kListHead;
+  int32_t* marks = free_list + kListHead + n_blocks;
+  int n_free = min(max(free_list[0], 0), n_blocks);
+  auto last_of = [&](int len) { return min(blocks_of(len, shift), max_blocks); };
+  int total = n_ids;
+  if (TABLE) {
+    uint32_t sum = 0;
+    for (int r0 = 0; r0 < n_b; r0 += kReturnThreads) {
+      const int r = r0 + tid, b = n_b - 1 - r;
+      uint32_t count = 0;
+      if (r < n_b) {
+        const int len = lens[b], cut = new_lens[b];
+        if (cut >= 0 && cut < len) count = (uint32_t)max(last_of(len) - blocks_of(cut, shift), 0);
+      }
+      uint32_t all;
+      const uint32_t end = scan_capped<kReturnThreads>(count, 0x7fffffffu, s_wave, all) + sum;
+      if (r < n_b) s_end[r] = (int)end;
+      sum += all;
+    }
+    __syncthreads();
+    total = (int)sum;
+  }
+  for (int p0 = 0; p0 < total; p0 += kReturnThreads * kPerThread) {
+    const int first = p0 + tid * kPerThread;
+    int id[kPerThread];
+    int row = TABLE && first < total ? owner_of(s_end, n_b, first) : 0;
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+      const int p = first + e;
+      id[e] = -1;
+      if (p < total) {
+        int64_t at = n_ids - 1 - p;
+        if (TABLE) {
+          while (s_end[row] <= p) ++row;
+          const int b = n_b - 1 - row;
+          at = (int64_t)b * max_blocks + last_of(lens[b]) - 1 - (p - (row ? s_end[row - 1] : 0));
+        }
+        id[e] = entries[at];
+        if (TABLE) entries[at] = -1;
+        if ((unsigned)id[e] >= (unsigned)n_blocks) id[e] = -1;
+        else atomicMin(&marks[id[e]], p);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0);         // the marks have been lowered
+    __syncthreads();
+    uint32_t mine = 0;
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+      if (id[e] >= 0 && __hip_atomic_load(&marks[id[e]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != first + e) id[e] = -1;
+      mine += id[e] >= 0;
+    }
+    uint32_t all;
+    int to = n_free + (int)(scan_capped<kReturnThreads>(mine, 0x7fffffffu, s_wave, all) - mine);   // (behind its barrier all marks have been read)
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e)
+      if (id[e] >= 0) {
+        if (to < n_blocks) stack[to] = id[e];
+        ++to;
+        __hip_atomic_store(&marks[id[e]], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    n_free = min(n_free + (int)all, n_blocks);
+    __builtin_amdgcn_s_waitcnt(0);         // (the next tile may hold the same blocks)
+    __syncthreads();
+  }
+  if (TABLE)
+    for (int b = tid; b < n_b; b += kReturnThreads) {
+      const int cut = new_lens[b];
+      if (cut >= 0 && cut < lens[b]) lens[b] = cut;
+    }
+  if (tid == 0) free_list[0] = n_free;
+}
+
+// Rows of k and v [n, heads, dim] into the pool by their slots (block * block_size + offset), degree 1; a slot outside the
+// pool is passed over.  Bound by its bytes: a thread takes 16-byte pieces, consecutive ones of a row, of both tensors.
+constexpr int kWriteThreads = 256, kWritePieces = 4;
+__global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
+    const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, int64_t row_stride, int64_t head_stride,
+    const int32_t* __restrict__ slots, int n, unsigned char* __restrict__ K_pool, unsigned char* __restrict__ V_pool,
+    int32_t* __restrict__ deg_pool, int heads, int pieces_per_row, int shift, int n_blocks, int rows_per_group) {
+  const int per_row = heads * pieces_per_row;
+  const int r0 = blockIdx.x * rows_per_group, r1 = min(r0 + rows_per_group, n);
+  for (int e = threadIdx.x; e < (r1 - r0) * per_row; e += kWriteThreads) {
+    const int r = r0 + e / per_row, x = e % per_row, h = x / pieces_per_row, piece = x % pieces_per_row;
+    const int slot = slots[r];
+    if (slot < 0 || (slot >> shift) >= n_blocks) continue;
+    const int64_t from = r * row_stride + h * head_stride + piece * 16;
+    const int64_t row = ((((int64_t)(slot >> shift) * heads + h) << shift) + (slot & ((1 << shift) - 1)));
+    const uint4 a = *reinterpret_cast<const uint4*>(k + from), c = *reinterpret_cast<const uint4*>(v + from);
+    *reinterpret_cast<uint4*>(K_pool + (row * pieces_per_row + piece) * 16) = a;
+    *reinterpret_cast<uint4*>(V_pool + (row * pieces_per_row + piece) * 16) = c;
+    if (piece == 0 && deg_pool) deg_pool[row] = 1;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_new, int32_t* free_list, int n_b, int max_blocks,
+                                int n_blocks, int shift, int32_t* slots, int n_slots, int32_t* starts, int32_t* granted,
+                                hipStream_t st) {
+  ScopedTimer t("paged_reserve", st);
+  const int groups = n_slots > kSlotsPerGroup ? div_up(n_slots, kSlotsPerGroup) : 1;
+  hipLaunchKernelGGL(paged_reserve_kernel, dim3((unsigned)groups), dim3(kReserveThreads), (size_t)n_b * 12, st, table, lens, n_new,
+                     free_list, n_b, max_blocks, n_blocks, shift, slots, n_slots, starts, granted);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int n_b, int max_blocks,
+                             int n_blocks, int shift, hipStream_t st) {
+  ScopedTimer t("paged_trim", st);
+  hipLaunchKernelGGL(paged_return_kernel<true>, dim3(1), dim3(kReturnThreads), (size_t)n_b * 4, st, table, 0, max_blocks, n_b, lens,
+                     new_lens, free_list, n_blocks, shift);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int n_blocks, hipStream_t st) {
+  if (n == 0) return hipSuccess;
+  ScopedTimer t("paged_free", st);
+  hipLaunchKernelGGL(paged_return_kernel<false>, dim3(1), dim3(kReturnThreads), 0, st, const_cast<int32_t*>(ids), n, 0, 0,
+                     static_cast<int32_t*>(nullptr), static_cast<const int32_t*>(nullptr), free_list, n_blocks, 0);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int n,
+                              void* K_pool, void* V_pool, int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
+                              hipStream_t st) {
+  if (n == 0) return hipSuccess;
+  ScopedTimer t("paged_write", st);
+  const int per_row = heads * (row_bytes / 16), most = kWriteThreads * kWritePieces;
+  const int rows = per_row < most ? most / per_row : 1;
+  hipLaunchKernelGGL(paged_write_kernel, dim3((unsigned)div_up(n, rows)), dim3(kWriteThreads), 0, st,
+                     static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), row_stride, head_stride, slots, n,
+                     static_cast<unsigned char*>(K_pool), static_cast<unsigned char*>(V_pool), deg_pool, heads, row_bytes / 16, shift,
+                     n_blocks, rows);
+  return hipGetLastError();
+}
+
+}  // namespace ckv
