@@ -374,9 +374,7 @@ int ckv_paged_bounds(const void* K_pool, const int32_t* deg_pool, const int32_t*
  *   sel int32 [batch, heads, n_select]: block * heads + head for the selected blocks in ascending order of
  *       position (-1 for one whose entry lies outside the pool), then -1.
  *   sel_lens int32 [batch, heads]: tokens in them.
- *   workspace: as for ckv_decode_attn, an int32 arrival counter per (sequence, KV head) comes first: zero-fill it
- *       once when it is allocated; every call leaves the counters zero.  The size for a max_len serves every smaller
- *       one; before a call with a larger batch * heads than it has served since, zero it again. */
+ *   workspace: scratch, whatever it holds; the size for a max_len serves every smaller one. */
 int ckv_paged_select_workspace(const ckv_paged_layout* pl, int32_t max_len, size_t* bytes);
 int ckv_paged_select(const void* q, int32_t q_heads, const void* bounds, const int32_t* mass, const int32_t* block_table,
                      const int32_t* lens, const ckv_paged_layout* pl, int32_t max_len, int32_t n_select, int32_t n_sink,

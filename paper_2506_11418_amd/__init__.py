@@ -684,8 +684,7 @@ def paged_select(q, bounds, mass, block_table, lens, max_len: int, n_select: int
                  n_recent: int = 1, scale: float = 0.0, out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None):
     """ckv_paged_select: the n_select blocks per (sequence, KV head) with the largest upper bound of softmax mass for q
     [batch, q_heads, dim], the first n_sink and last n_recent always among them: (sel [batch, heads, n_select], sel_lens
-    [batch, heads]) for paged_sparse_decode_attn.  `out` may pass both; a `workspace` passed in must have been zero-filled when
-    it was allocated."""
+    [batch, heads]) for paged_sparse_decode_attn.  `out` may pass both, `workspace` scratch of paged_select_workspace() bytes."""
     if out is not None and workspace is not None and q.is_cuda:
         st = (_native or _binding()).paged_select(q, bounds, mass, block_table, lens, max_len, n_select, block_size, n_sink, n_recent,
                                                   scale, *out, workspace, *_here())
@@ -710,7 +709,7 @@ def paged_select(q, bounds, mass, block_table, lens, max_len: int, n_select: int
     _ints("sel", sel, B, H, n_select)
     _ints("sel_lens", sel_lens, B, H)
     if workspace is None:
-        workspace = torch.zeros(paged_select_workspace(pl, max_len), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(paged_select_workspace(pl, max_len), dtype=torch.uint8, device=q.device)
     _on_this_gpu(q, bounds, mass, block_table, lens, sel, sel_lens, workspace)
     st = lib().ckv_paged_select(_ptr(q), q_heads, _ptr(bounds), _ptr(mass), _ptr(block_table), _ptr(lens), C.byref(pl), max_len,
                                 n_select, n_sink, n_recent, scale, _ptr(sel), _ptr(sel_lens), _ptr(workspace),

@@ -992,7 +992,7 @@ int ckv_paged_select_workspace(const ckv_paged_layout* pl, int32_t max_len, size
   if (!bytes) return CKV_EINVAL;
   if (max_len <= 0) return CKV_ESHAPE;
   const size_t rows = (size_t)pl->batch * pl->heads;
-  *bytes = ckv::align_up(ckv::attn_counter_bytes(pl->batch, pl->heads) + rows * key_stride(pl, max_len) * sizeof(uint32_t), 256);
+  *bytes = ckv::align_up(rows * ckv::select_words(key_stride(pl, max_len)) * sizeof(uint32_t), 256);
   return CKV_OK;
 }
 
@@ -1024,8 +1024,7 @@ int ckv_paged_select(const void* q, int32_t q_heads, const void* bounds, const i
   c.n_b = pl->batch; c.heads = pl->heads; c.dim = pl->dim;
   c.n_select = n_select; c.n_sink = n_sink; c.n_recent = n_recent;
   c.scale = scale;
-  c.arrived = static_cast<int32_t*>(workspace);
-  c.keys = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + ckv::attn_counter_bytes(pl->batch, pl->heads));
+  c.keys = static_cast<uint32_t*>(workspace);
   c.key_stride = key_stride(pl, max_len);
   c.sel = sel; c.sel_lens = sel_lens;
   c.st = static_cast<hipStream_t>(hip_stream);

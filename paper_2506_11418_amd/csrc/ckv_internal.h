@@ -229,12 +229,21 @@ struct SelectCall {
   const int32_t* lens;
   int max_len, n_b, heads, dim, n_select, n_sink, n_recent;
   float scale;
-  int32_t* arrived;       // a counter a (sequence, head), zero between calls
-  uint32_t* keys;         // [n_b, heads, key_stride]: a rank a block
+  uint32_t* keys;         // [n_b, heads, key_stride]: a rank a block; then, for long rows, what their segments keep
   int key_stride;
   int32_t *sel, *sel_lens;
   hipStream_t st;
+  // set by the launch: segments of a long row, and [n_b, heads, 2, segments, most]: the keys and blocks each keeps
+  uint32_t* kept;
+  int segment, segments, most;
 };
+constexpr int kSelectSegment = 2048, kSelectMost = 512;
+// rows that are cut into segments: long ones of which few blocks are wanted
+inline bool select_in_segments(int key_stride, int most) { return key_stride > 4 * kSelectSegment && most > 0 && most <= kSelectMost; }
+// 32-bit words of scratch for a row
+inline size_t select_words(int key_stride) {
+  return (size_t)key_stride + (select_in_segments(key_stride, 1) ? (size_t)2 * kSelectMost * div_up(key_stride, kSelectSegment) : 0);
+}
 hipError_t launch_paged_select(int dtype, int G, const SelectCall& c);
 
 // ---- timing hooks ----------------------------------------------------------------------------

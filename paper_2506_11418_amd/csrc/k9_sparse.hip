@@ -67,8 +67,8 @@ __global__ __launch_bounds__(kBoundsThreads) void paged_bounds_kernel(const T* _
 }
 
 // Ranks, largest first: a score that is no finite fp32 number, the scores, a block without tokens that count or outside the pool.
-// No rank is 0xffffffff.
-constexpr uint32_t kNotFinite = 0xfffffffeu, kNothing = 0u;
+// No rank is 0: that is no block at all.
+constexpr uint32_t kNotFinite = 0xffffffffu, kNothing = 1u;
 
 // The score in 64 bits, rounded once to fp32.  In 32 bits the order of close scores would hang on the order of the sums, and
 // neighbours at the cut are close: a selection among 2048 blocks has one chance in some hundred to come out differently.
@@ -90,24 +90,32 @@ __device__ __forceinline__ uint32_t rank_of(double dot, double scale, int mass) 
 template <typename T, int D, int G>
 struct ScoreTile {
   static constexpr int E = 16 / sizeof(T);                 // bounds in a piece
-  static constexpr int L = 2 * D / E / 4;                  // pieces of a lane
+  static constexpr int PIECES = 2 * D / E;                 // of a block's row
+  static constexpr int L = PIECES / 4;                     // of a lane
   static constexpr int SETS = G > 4 ? 2 : 1;               // of four heads
-  static constexpr bool AHEAD = 4 * L * (2 + SETS * E / 4) <= 160;   // registers for the next tile while one is worked on
+  static constexpr int BYTES = 16 * PIECES * 16;           // of a tile in LDS
+  // byte offset of a piece of a tile's row in LDS: the XOR spreads the 16 rows of one piece column over all banks
+  __device__ static int lds(int row, int piece) { return (row * PIECES + (piece ^ (row & 7))) << 4; }
 };
 constexpr int kScoreThreads = 256, kScoreWaves = kScoreThreads / 64;
+// waves a SIMD: the queries of eight heads of 128 channels, or an fp32 tile of them, take the registers of two; both of four
 template <typename T, int D, int G>
-__global__ __launch_bounds__(kScoreThreads, 2) void paged_score_kernel(const T* __restrict__ q, const T* __restrict__ bounds,
+constexpr int score_waves() { return sizeof(T) * D * (G > 4 ? 2 : 1) >= 1024 ? 1 : sizeof(T) * D * (G > 4 ? 2 : 1) >= 512 ? 2 : 3; }
+template <typename T, int D, int G>
+__global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged_score_kernel(const T* __restrict__ q, const T* __restrict__ bounds,
                                                                        const int32_t* __restrict__ mass, PagedView paged,
                                                                        const int32_t* __restrict__ lens, int max_len, int heads,
                                                                        int n_select, int n_sink, int n_recent, float scale,
                                                                        uint32_t* __restrict__ keys, int key_stride) {
   typedef ScoreTile<T, D, G> S;
   constexpr int E = S::E, L = S::L;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y, b = blockIdx.z;
+  __shared__ __attribute__((aligned(16))) unsigned char s_tile[kScoreWaves * S::BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), b = blockIdx.y;
   const int n = div_up(max(min(lens[b], max_len), 0), 1 << paged.shift);
+  const int unit = blockIdx.x * kScoreWaves + wave, h = unit % heads, waves = gridDim.x * kScoreWaves / heads;   // of one head
   const int lo = n_sink, hi = n - n_recent;                // the blocks to rank
-  const int first = (lo / 16 + blockIdx.x * kScoreWaves + wave) * 16, step = gridDim.x * kScoreWaves * 16;
-  if (n <= n_select || first >= hi) return;
+  const int first = (lo / 16 + unit / heads) * 16, step = waves * 16;
+  if (n <= n_select || first >= hi || unit >= waves * heads) return;
   const int row = lane & 15, k = lane >> 4;
   const int32_t* table = paged.table + (int64_t)b * paged.max_blocks;
 
@@ -123,32 +131,46 @@ __global__ __launch_bounds__(kScoreThreads, 2) void paged_score_kernel(const T* 
       for (int e = 0; e < E; ++e) qv[s][j][e] = at < D ? fminf((float)p.x[e], 0.f) : fmaxf((float)p.x[e], 0.f);
     }
 
+  unsigned char* tile = s_tile + wave * S::BYTES;
   struct Tile {
     uint4 v[L];
-    int mass;          // 0 for a block outside the pool
+    int mass;          // of block `row`; 0 outside the pool
   };
   auto id_of = [&](int i0) { return table[min(i0 + row, hi - 1)]; };
+  // whole rows, consecutive lanes consecutive pieces (lane block + 16 piece straight from memory takes a row of cache tags for every four
+  // lanes: 268 MB 80 us, so 69), read once and not kept: the caches have better use for their room (with ordinary loads 166 us)
   auto issue = [&](Tile& t, int blk) {
     const bool in = (unsigned)blk < (unsigned)paged.n_blocks;
-    const int64_t slab = (int64_t)(in ? blk : 0) * heads + h;
+    const int slab = (in ? blk : 0) * heads + h;
     t.mass = mass[slab];
-    const char* p = reinterpret_cast<const char*>(bounds + slab * (2 * D)) + k * 16;
 #pragma unroll
-    for (int j = 0; j < L; ++j) t.v[j] = ldg16_stream(p + j * 64);
+    for (int j = 0; j < L; ++j) {
+      const int at = 64 * j + lane;
+      t.v[j] = ldg16_stream(bounds + (int64_t)__shfl(slab, at / S::PIECES) * (2 * D) + at % S::PIECES * E);
+    }
     t.mass = in ? t.mass : 0;
   };
-  auto work = [&](const Tile& t, int i0) {
-    if constexpr (S::SETS == 2)                            // eight heads in 64 bits do not fit the registers: widened every time
+  auto stage = [&](const Tile& t) {
 #pragma unroll
-      for (int s = 0; s < S::SETS; ++s)
+    for (int j = 0; j < L; ++j) {
+      const int at = 64 * j + lane;
+      *reinterpret_cast<uint4*>(tile + S::lds(at / S::PIECES, at % S::PIECES)) = t.v[j];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // other lanes' pieces are read next (a wave's accesses to LDS are in order)
+  };
+  auto work = [&](int tile_mass, int i0) {
+    // (held in 64 bits for the whole loop they would take a third wave's registers, or spill)
 #pragma unroll
-        for (int j = 0; j < L; ++j)
+    for (int s = 0; s < S::SETS; ++s)
 #pragma unroll
-          for (int e = 0; e < E; ++e) asm volatile("" : "+v"(qv[s][j][e]));
+      for (int j = 0; j < L; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) asm volatile("" : "+v"(qv[s][j][e]));
     double acc[S::SETS][2] = {};
 #pragma unroll
     for (int j = 0; j < L; ++j) {
-      const uint32_t w[4] = {t.v[j].x, t.v[j].y, t.v[j].z, t.v[j].w};
+      const uint4 v = *reinterpret_cast<const uint4*>(tile + S::lds(row, 4 * j + k));
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         float x;
@@ -159,6 +181,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void paged_score_kernel(const T* 
           acc[s][e & 1] = __builtin_amdgcn_mfma_f64_4x4x4f64((double)x, (double)qv[s][j][e], acc[s][e & 1], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     auto finite = [](double x) { return x - x == 0. ? x : (double)INFINITY; };
     double best = finite(acc[0][0] + acc[0][1]);
     if constexpr (S::SETS == 2) best = fmax(best, finite(acc[1][0] + acc[1][1]));
@@ -171,45 +194,36 @@ __global__ __launch_bounds__(kScoreThreads, 2) void paged_score_kernel(const T* 
     across(std::integral_constant<int, 0xB1>{});
     across(std::integral_constant<int, 0x4E>{});
     const int out = (lane >> 4) + (lane & 12);             // the block of this lane's D
-    const int m = __shfl(t.mass, out), i = i0 + out;
+    const int m = __shfl(tile_mass, out), i = i0 + out;
     const uint32_t key = m > 0 ? rank_of(best, (double)scale, m) : kNothing;
     if ((lane & 3) == 0 && i >= lo && i < hi) keys[((int64_t)b * heads + h) * key_stride + i] = key;
   };
   // table entries are read two tiles ahead, bounds one
-  Tile ta, tb;
+  Tile t;
   int next = id_of(first + step);
-  issue(ta, id_of(first));
-  if constexpr (S::AHEAD) {
-    for (int i0 = first;; i0 += 2 * step) {
-      const int blk = next;
-      next = id_of(i0 + 2 * step);
-      if (i0 + step < hi) issue(tb, blk);
-      work(ta, i0);
-      if (i0 + step >= hi) break;
-      const int blk2 = next;
-      next = id_of(i0 + 3 * step);
-      if (i0 + 2 * step < hi) issue(ta, blk2);
-      work(tb, i0 + step);
-      if (i0 + 2 * step >= hi) break;
-    }
-  } else {
-    for (int i0 = first;;) {
-      work(ta, i0);
-      i0 += step;
-      if (i0 >= hi) break;
-      issue(ta, next);
-      next = id_of(i0 + step);
-    }
+  issue(t, id_of(first));
+  for (int i0 = first;; i0 += step) {
+    const int m = t.mass;
+    stage(t);
+    if (i0 + step < hi) issue(t, next);
+    next = id_of(i0 + 2 * step);
+    work(m, i0);
+    if (i0 + step >= hi) break;
   }
 }
 
-// The n_select blocks of a (sequence, KV head) to read, in ascending order: the always selected ones and the largest keys of the
-// others, ties to the lower block.  A thread holds KEYS keys (rows of more than that are read again for every step).
+// The blocks of a (sequence, KV head) to read, in ascending order: the always selected ones and the largest keys of the others,
+// ties to the lower block.  A thread holds KEYS keys (rows of more than that are read again for every step).
 //
 // The cut is found by histograms of kBins bins of equal width between the least and the largest key: then inside the bin that
 // holds it, until that bin is wholly taken or is one key.  Scores lie close together in their exponents, so that
 // digits from the top would put most of them into a few bins, whose counters are then bumped one lane at a time.
-// Places follow from ballots: 64 neighbouring blocks are a word of a bit mask.
+// Places follow from ballots: 64 neighbouring keys are a word of a bit mask.
+//
+// One CU takes half a microsecond for every instruction that 65536 keys need, so that long rows are cut into segments: a
+// workgroup each finds the keys of its segment that can be among the largest, and one more takes the cut among those
+// (65536 blocks of 8 heads, 256 of them: 49 us in one step).
+enum class Step { WHOLE, SEGMENT, JOIN };
 constexpr int kBins = 2048;
 template <int THREADS>
 __device__ __forceinline__ int scan_int(int x, int* s_wave, int& all) {
@@ -227,55 +241,88 @@ __device__ __forceinline__ int scan_int(int x, int* s_wave, int& all) {
   __syncthreads();
   return x + before;
 }
-template <int THREADS, int KEYS>
-__global__ __launch_bounds__(THREADS) void paged_select_kernel(const uint32_t* __restrict__ keys, int key_stride, PagedView paged,
-                                                               const int32_t* __restrict__ lens, int max_len, int heads,
-                                                               int n_select, int n_sink, int n_recent, int32_t* __restrict__ sel,
-                                                               int32_t* __restrict__ sel_lens) {
+template <int THREADS, int KEYS, Step STEP>
+__global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
   constexpr int W = THREADS / 64, SPAN = THREADS * KEYS, WORDS = SPAN / 64;
-  __shared__ int s_hist[kBins], s_wave[W], s_found[3];
+  __shared__ int s_hist[kBins], s_wave[W], s_found[3], s_end;     // s_end: the last block is taken
   __shared__ uint32_t s_range[2];
   __shared__ uint64_t s_mask[WORDS];
   __shared__ int s_before[WORDS];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.x, b = blockIdx.y;
-  const int len = max(min(lens[b], max_len), 0), bs = 1 << paged.shift, n = div_up(len, bs);
-  const int64_t bh = (int64_t)b * heads + h;
-  const uint32_t* key = keys + bh * key_stride;
-  const int32_t* table = paged.table + (int64_t)b * paged.max_blocks;
-  int32_t* out = sel + bh * n_select;
-  auto put = [&](int place, int i) {
-    const int blk = table[i];
-    out[place] = (unsigned)blk < (unsigned)paged.n_blocks ? blk * heads + h : -1;
+  const int64_t bh = (int64_t)b * c.heads + h;
+  const int32_t* table = c.paged.table + (int64_t)b * c.paged.max_blocks;
+  const int32_t* other = nullptr;                // JOIN: the blocks the keys belong to
+  const uint32_t* key = c.keys + bh * c.key_stride;
+  int row = c.key_stride;                        // readable keys
+  if constexpr (STEP == Step::SEGMENT) {
+    key += blockIdx.z * SPAN;
+    row -= blockIdx.z * SPAN;
+  }
+  if constexpr (STEP == Step::JOIN) {
+    key = c.kept + bh * c.segments * c.most * 2;
+    other = reinterpret_cast<const int32_t*>(key) + c.segments * c.most;
+    row = c.segments * c.most;
+  }
+  // The first span's keys, and what they stand for where there are few, are on their way before the length is known: what lies behind it
+  // is read and not looked at.  No load is behind a branch.
+  constexpr bool kFew = KEYS <= 8 && STEP != Step::SEGMENT;
+  uint32_t x[KEYS];
+  int entry[kFew ? KEYS : 1];
+  auto load = [&](int span) {
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) x[j] = key[min(span * SPAN + j * THREADS + tid, row - 1)];
   };
-  if (n <= n_select) {
-    for (int i = tid; i < n_select; i += THREADS) {
-      if (i < n) put(i, i);
-      else out[i] = -1;
-    }
-    if (tid == 0) sel_lens[bh] = len;
+  load(0);
+  if constexpr (kFew) {
+#pragma unroll
+    for (int j = 0; j < KEYS; ++j) entry[j] = (STEP == Step::JOIN ? other : table)[min(j * THREADS + tid, row - 1)];
+  }
+  const int bs = 1 << c.paged.shift, len = max(min(c.lens[b], c.max_len), 0), n = div_up(len, bs);
+  auto named = [&](int blk) { return (unsigned)blk < (unsigned)c.paged.n_blocks ? blk * c.heads + h : -1; };
+  int32_t* out = c.sel + bh * c.n_select;
+  if (n <= c.n_select) {
+    if (STEP == Step::SEGMENT) return;
+    for (int i = tid; i < c.n_select; i += THREADS) out[i] = i < n ? named(table[i]) : -1;
+    if (tid == 0) c.sel_lens[bh] = len;
     return;
   }
-  const int lo_i = n_sink, hi_i = n - n_recent, spans = div_up(n, SPAN);
-  uint32_t x[KEYS];
-  auto load = [&](int span) {
+  // which keys count: [lo, hi) of the row
+  int lo = c.n_sink, hi = n - c.n_recent, want = c.n_select - c.n_sink - c.n_recent;
+  if constexpr (STEP == Step::SEGMENT) {
+    const int at = blockIdx.z * SPAN;
+    if (at >= n) return;                         // (not looked at by the last step)
+    lo = min(max(lo - at, 0), SPAN);
+    hi = min(max(hi - at, lo), SPAN);
+    want = min(want, hi - lo);
+  }
+  if constexpr (STEP == Step::JOIN) {
+    lo = 0;
+    hi = div_up(n, c.segment) * c.most;
+  }
+  const int spans = max(div_up(hi, SPAN), 1);
+  auto counted = [&](int span) {                 // 0 for keys that do not count
 #pragma unroll
     for (int j = 0; j < KEYS; ++j) {
       const int i = span * SPAN + j * THREADS + tid;
-      x[j] = i >= lo_i && i < hi_i ? key[i] : 0u;
+      x[j] = (unsigned)(i - lo) < (unsigned)(hi - lo) ? x[j] : 0u;
     }
   };
-  auto ranked = [&](int span, int j) { const int i = span * SPAN + j * THREADS + tid; return i >= lo_i && i < hi_i; };
+  counted(0);
+  auto each_span = [&](auto&& f) __attribute__((always_inline)) {
+    for (int span = 0; span < spans; ++span) {
+      if (spans > 1) { load(span); counted(span); }
+      f(span);
+    }
+  };
   // the range of the keys
-  if (tid == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0u; s_found[0] = 0; }
+  if (tid == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0u; s_end = 0; }
   __syncthreads();
   {
-    uint32_t least_key = 0xffffffffu, most_key = 0u;
-    for (int span = 0; span < spans; ++span) {
-      load(span);
+    uint32_t least_key = 0xffffffffu, most_key = 0u;         // (of the key below: 0 becomes the largest)
+    each_span([&](int) {
 #pragma unroll
-      for (int j = 0; j < KEYS; ++j)
-        if (ranked(span, j)) { least_key = min(least_key, x[j]); most_key = max(most_key, x[j]); }
-    }
+      for (int j = 0; j < KEYS; ++j) { least_key = min(least_key, x[j] - 1); most_key = max(most_key, x[j]); }
+    });
     for (int w = 1; w < 64; w *= 2) {
       least_key = min(least_key, (uint32_t)__shfl_xor((int)least_key, w));
       most_key = max(most_key, (uint32_t)__shfl_xor((int)most_key, w));
@@ -283,21 +330,20 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(const uint32_t* _
     if (lane == 0) { atomicMin(&s_range[0], least_key); atomicMax(&s_range[1], most_key); }
   }
   __syncthreads();
-  uint32_t from = s_range[0], to = s_range[1];   // the cut lies in [from, to]; what is above `to` is taken
-  int want = n_select - n_sink - n_recent;       // of the keys in it, counted from the top
+  uint32_t from = s_range[0] + 1, to = s_range[1];           // the cut lies in [from, to]; what is above `to` is taken
   bool whole = false;                            // all of them
-  if (want == 0) from = to = 0xffffffffu;        // (no key is that large)
-  while (want > 0) {
+  const bool none = want == 0;
+  int left = want;                               // to be taken in [from, to], counted from the top
+  while (left > 0) {
     const uint32_t width = to - from;
     const int shift = width < kBins ? 0 : 32 - __clz(width) - 11;
     for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
     __syncthreads();
-    for (int span = 0; span < spans; ++span) {
-      if (spans > 1) load(span);
+    each_span([&](int) {
 #pragma unroll
       for (int j = 0; j < KEYS; ++j)
-        if (ranked(span, j) && x[j] >= from && x[j] <= to) atomicAdd(&s_hist[(x[j] - from) >> shift], 1);
-    }
+        if (x[j] - from <= width) atomicAdd(&s_hist[(x[j] - from) >> shift], 1);
+    });
     __syncthreads();
     constexpr int PER = kBins / THREADS;         // a thread's bins, in falling order
     int count[PER], mine = 0, all;
@@ -306,24 +352,23 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(const uint32_t* _
     int upto = scan_int<THREADS>(mine, s_wave, all) - mine;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (upto < want && upto + count[i] >= want) { s_found[0] = kBins - 1 - (tid * PER + i); s_found[1] = want - upto; s_found[2] = count[i]; }
+      if (upto < left && upto + count[i] >= left) { s_found[0] = kBins - 1 - (tid * PER + i); s_found[1] = left - upto; s_found[2] = count[i]; }
       upto += count[i];
     }
     __syncthreads();
     const uint32_t base = from + ((uint32_t)s_found[0] << shift);
     to = base + min(to - base, (1u << shift) - 1);
     from = base;
-    want = s_found[1];
-    whole = want == s_found[2];
+    left = s_found[1];
+    whole = left == s_found[2];
     __syncthreads();                             // (s_found and s_hist are free again)
     if (whole || from == to) break;
   }
-  // places: the blocks before a word of 64, and in it
+  // places: the keys taken before a word of 64, and in it
   int at = 0, tied = 0;
-  for (int span = 0; span < spans; ++span) {
-    if (spans > 1) load(span);
-    const int words = min(WORDS, div_up(n - span * SPAN, 64));
-    auto places = [&](auto&& test, int& before_all) {      // s_mask and s_before of the blocks that pass the test
+  each_span([&](int span) {
+    const int words = min(WORDS, max(div_up(hi - span * SPAN, 64), 0));
+    auto places = [&](auto&& test, int& before_all) {        // s_mask and s_before of the keys that pass the test
 #pragma unroll
       for (int j = 0; j < KEYS; ++j) {
         const uint64_t m = __ballot(test(j));
@@ -332,46 +377,59 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(const uint32_t* _
       __syncthreads();
       for (int w0 = 0; w0 < words; w0 += THREADS) {
         const int w = w0 + tid;
-        const int c = w < words ? __popcll(s_mask[w]) : 0;
+        const int n_in = w < words ? __popcll(s_mask[w]) : 0;
         int all;
-        const int upto = scan_int<THREADS>(c, s_wave, all);
-        if (w < words) s_before[w] = before_all + upto - c;
+        const int upto = scan_int<THREADS>(n_in, s_wave, all);
+        if (w < words) s_before[w] = before_all + upto - n_in;
         before_all += all;
       }
       __syncthreads();
     };
     auto place_of = [&](int j) { return s_before[j * W + wave] + (int)__popcll(s_mask[j * W + wave] & ((1ull << lane) - 1)); };
-    uint64_t first_ties = ~0ull;                 // bit j: this thread's j-th key, if it equals the cut, is taken
-    if (!whole) {
-      places([&](int j) { return ranked(span, j) && x[j] == from; }, tied);
+    if (!whole && !none) {                       // of the keys that equal the cut the first ones; the others count no longer
+      places([&](int j) { return x[j] == from; }, tied);
 #pragma unroll
       for (int j = 0; j < KEYS; ++j)
-        if (place_of(j) >= want) first_ties &= ~(1ull << j);
+        if (x[j] == from && place_of(j) >= left) x[j] = 0;
       __syncthreads();                           // (read before the next ones are written)
     }
-    auto taken = [&](int j) {
-      const int i = span * SPAN + j * THREADS + tid;
-      return i < n && (i < lo_i || i >= hi_i || (whole ? x[j] >= from : x[j] > from || (x[j] == from && (first_ties >> j & 1))));
-    };
+    auto taken = [&](int j) { return !none && x[j] >= from && x[j] != 0; };
     places(taken, at);
 #pragma unroll
     for (int j = 0; j < KEYS; ++j)
       if (taken(j)) {
-        const int i = span * SPAN + j * THREADS + tid;
-        put(place_of(j), i);
-        if (i == n - 1) s_found[0] = -1;
+        const int i = span * SPAN + j * THREADS + tid, to_place = place_of(j);
+        if constexpr (STEP == Step::SEGMENT) {
+          uint32_t* kept = c.kept + (bh * c.segments * 2 + blockIdx.z) * c.most + to_place;
+          kept[0] = x[j];
+          kept[c.segments * c.most] = (uint32_t)(blockIdx.z * SPAN + i);
+        } else {
+          int blk = entry[kFew ? j : 0];
+          if (!kFew || spans > 1) blk = STEP == Step::JOIN ? other[i] : table[i];
+          if ((STEP == Step::JOIN ? blk : i) == n - 1) s_end = 1;
+          out[c.n_sink + to_place] = named(STEP == Step::JOIN ? table[blk] : blk);
+        }
       }
     __syncthreads();
+  });
+  if constexpr (STEP == Step::SEGMENT) {
+    uint32_t* kept = c.kept + (bh * c.segments * 2 + blockIdx.z) * c.most;
+    for (int i = at + tid; i < c.most; i += THREADS) kept[i] = 0u;
+  } else {
+    for (int i = tid; i < c.n_sink + c.n_recent; i += THREADS) {
+      const int place = i < c.n_sink ? i : i - c.n_sink + c.n_select - c.n_recent;
+      out[place] = named(table[i < c.n_sink ? i : i - c.n_sink + n - c.n_recent]);
+    }
+    if (tid == 0) c.sel_lens[bh] = c.n_select * bs - (c.n_recent > 0 || s_end ? n * bs - len : 0);   // (the last block may be short)
   }
-  if (tid == 0) sel_lens[bh] = n_select * bs - (s_found[0] == -1 ? n * bs - len : 0);
 }
 
 template <typename T, int D, int G>
 hipError_t launch_scores(const SelectCall& c) {
-  // four waves a workgroup; as many workgroups as run at once (two a CU at least), as long as every wave has a tile
-  const int tiles = div_up(c.key_stride, 16 * kScoreWaves), pairs = c.n_b * c.heads;
-  const int fit = div_up(4 * cu_count(), pairs);
-  hipLaunchKernelGGL((paged_score_kernel<T, D, G>), dim3((unsigned)(tiles < fit ? tiles : fit), (unsigned)c.heads, (unsigned)c.n_b),
+  // waves that run at once, as long as each has a tile, and whole heads
+  const int tiles = div_up(c.key_stride, 16), fit = div_up(3 * kScoreWaves * cu_count(), c.n_b * c.heads);
+  const int waves = (tiles < fit ? tiles : fit) * c.heads;
+  hipLaunchKernelGGL((paged_score_kernel<T, D, G>), dim3((unsigned)div_up(waves, kScoreWaves), (unsigned)c.n_b),
                      dim3(kScoreThreads), 0, c.st, static_cast<const T*>(c.q), static_cast<const T*>(c.bounds), c.mass, c.paged, c.lens,
                      c.max_len, c.heads, c.n_select, c.n_sink, c.n_recent, c.scale, c.keys, c.key_stride);
   return hipGetLastError();
@@ -386,10 +444,10 @@ hipError_t launch_scores_g(int G, const SelectCall& c) {
   }
   return hipErrorInvalidValue;
 }
-template <int THREADS, int KEYS>
+template <int THREADS, int KEYS, Step STEP>
 hipError_t launch_select(const SelectCall& c) {
-  hipLaunchKernelGGL((paged_select_kernel<THREADS, KEYS>), dim3((unsigned)c.heads, (unsigned)c.n_b), dim3(THREADS), 0, c.st, c.keys, c.key_stride,
-                     c.paged, c.lens, c.max_len, c.heads, c.n_select, c.n_sink, c.n_recent, c.sel, c.sel_lens);
+  hipLaunchKernelGGL((paged_select_kernel<THREADS, KEYS, STEP>), dim3((unsigned)c.heads, (unsigned)c.n_b, (unsigned)(STEP == Step::SEGMENT ? c.segments : 1)),
+                     dim3(THREADS), 0, c.st, c);
   return hipGetLastError();
 }
 
@@ -421,10 +479,20 @@ hipError_t launch_paged_select(int dtype, int G, const SelectCall& c) {
            : c.dim == 32 ? launch_scores_g<float, 32>(G, c) : e;
     if (e != hipSuccess) return e;
   }
+  SelectCall s = c;
+  s.segment = kSelectSegment;
+  s.segments = div_up(c.key_stride, kSelectSegment);
+  s.most = c.n_select - c.n_sink - c.n_recent;
+  s.kept = c.keys + (int64_t)c.n_b * c.heads * c.key_stride;
   ScopedTimer t("paged_select", c.st);
-  if (c.key_stride <= 2048) return launch_select<256, 8>(c);
-  if (c.key_stride <= 16384) return launch_select<1024, 16>(c);
-  return launch_select<1024, 32>(c);
+  if (select_in_segments(c.key_stride, s.most)) {
+    e = launch_select<256, kSelectSegment / 256, Step::SEGMENT>(s);
+    if (e != hipSuccess) return e;
+    return s.segments * s.most <= 4096 ? launch_select<512, 8, Step::JOIN>(s) : launch_select<1024, 16, Step::JOIN>(s);
+  }
+  if (c.key_stride <= 2048) return launch_select<256, 8, Step::WHOLE>(s);
+  if (c.key_stride <= 8192) return launch_select<1024, 8, Step::WHOLE>(s);
+  return launch_select<1024, 16, Step::WHOLE>(s);
 }
 
 }  // namespace ckv

@@ -141,6 +141,9 @@ CASES = [
     ("bf16", 3, 8, 128, 1, [257, 64], 63, 5, 9, True), ("f32", 4, 2, 64, 32, [9001, 4500], 48, 1, 1, True),
     ("f32", 1, 4, 32, 16, [700, 33], 1, 0, 1, False), ("f32", 2, 8, 128, 16, [1111], 16, 1, 0, True), ("f32", 2, 1, 32, 4, [50], 12, 12, 0, True),
     ("bf16", 1, 2, 128, 16, [70000], 256, 1, 1, False), ("bf16", 33, 4, 64, 16, [400, 200], 9, 1, 1, True), ("bf16", 1, 1, 64, 2, [30011], 999, 3, 3, True),
+    # long rows: cut into segments, few and many kept, short sequences among them; and one wanted too many of for that
+    ("f32", 2, 2, 32, 1, [20000, 9, 2049, 4096], 7, 2, 0, False), ("bf16", 1, 4, 64, 1, [33333, 15000], 514, 1, 1, True),
+    ("f32", 1, 1, 32, 1, [40001], 600, 0, 1, False), ("f32", 1, 1, 32, 2, [30000], 6, 4, 2, True),
 ]
 
 
@@ -233,6 +236,24 @@ def test_ranks_of_equal_missing_and_infinite_scores():
     torch.cuda.synchronize()
     _, _, picked = c.want_select(q, bounds.cpu(), mass.cpu(), 640, 39, 1, 1, _scale(64))
     _check_attention(c, q, o, picked, 640, _scale(64))
+
+
+@pytest.mark.parametrize("tokens,n_select", [(300, 40), (12000, 100), (12000, 300), (12000, 700)])
+def test_ties_over_long_rows_go_to_the_lower_blocks(tokens, n_select):
+    """Blocks of one token with few different keys: the cut falls among many equal scores, in every form the selection takes."""
+    g = torch.Generator().manual_seed(n_select)
+    some = torch.randn(5, 32, generator=g)
+    c = Cache(15, [tokens, tokens // 3], 1, 32, 1, "f32", degrees=False)
+    for b, n in enumerate(c.lens):
+        c.K[c.table[b, :n].long(), 0, 0] = some[torch.randint(0, 5, (n,), generator=g)]
+    q = _queries(10, 2, 2, 32, "f32")
+    K, V, deg, table, n = c.gpu()
+    bounds, mass = ckv.paged_bounds(K, deg, table, n, tokens)
+    for n_sink, n_recent in ((0, 0), (1, 1), (n_select, 0), (0, n_select)):
+        sel, sel_lens = ckv.paged_select(q.to(DEV), bounds, mass, table, n, tokens, n_select, 1, n_sink, n_recent)
+        torch.cuda.synchronize()
+        want, count, _ = c.want_select(q, bounds.cpu(), mass.cpu(), tokens, n_select, n_sink, n_recent, _scale(32))
+        assert np.array_equal(i64(sel), want) and np.array_equal(i64(sel_lens), count), (n_sink, n_recent)
 
 
 def test_outputs_of_the_cache_type_and_by_either_route(monkeypatch):
