@@ -53,13 +53,34 @@ __device__ __forceinline__ int owner_of(const int32_t* end, int n, int x) {
   return lo;
 }
 
-constexpr int kReserveThreads = 256, kSlotsPerGroup = 1024;
+// the same for E values at once (n - 1 where there is none): their reads of LDS go together
+template <int E>
+__device__ __forceinline__ void owners_of(const int32_t* end, int n, const int (&x)[E], int (&at)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) at[e] = 0;
+  for (int step = 1 << (31 - __clz(n)); step > 0; step >>= 1) {
+    int v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = end[min(at[e] + step, n) - 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) at[e] += at[e] + step <= n && v[e] <= x[e] ? step : 0;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) at[e] = min(at[e], n - 1);
+}
+
+constexpr int kReserveThreads = 256;
 
 // Every workgroup works out for itself who gets what (two running sums over the requests, in LDS), then writes its share of
 // the slots and of the table entries: a request's j-th new token is token L + j of its row, in the entry the row has there
 // already or in one that this call deals, the i-th block dealt being the i-th from the stack's top.  Nothing that one workgroup
 // writes is read by another: lengths and the number of free blocks change when the last one has read them.
+//
+// What bounds it: a chain of trips to memory (lengths; entry or stack; store), for 64 requests of one token each the whole of its 3.5 us.
+// So a thread takes ROWS requests in a row (1000 requests, one and a pair of sums at a time: 12.3 us) and asks for the
+// entries of its slots together (135000 slots, one after the other: 8.8 us).
 // dynamic LDS: 12 bytes a request
+template <int ROWS, int SLOTS>   // a thread's requests and slots
 __global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
     int32_t* __restrict__ table, int32_t* __restrict__ lens, const int32_t* __restrict__ n_new, int32_t* __restrict__ free_list,
     int n_b, int max_blocks, int n_blocks, int shift, int32_t* __restrict__ slots, int n_slots, int32_t* __restrict__ starts,
@@ -67,54 +88,104 @@ __global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
   extern __shared__ int32_t s_dyn[];
   int32_t *s_end = s_dyn, *s_dealt = s_dyn + n_b, *s_len = s_dyn + 2 * n_b;   // sums up to each request; its length, -1: refused
   __shared__ uint32_t s_wave[kReserveThreads / 64];
-  __shared__ int s_take, s_last;
-  const int tid = threadIdx.x;
+  __shared__ int s_last;
+  const int tid = threadIdx.x, b0 = tid * ROWS;
+  int len[ROWS], fresh[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    len[r] = lens[min(b0 + r, n_b - 1)];
+    fresh[r] = n_new[min(b0 + r, n_b - 1)];
+  }
   const int n_free = min(max(free_list[0], 0), n_blocks);
   const int32_t* stack = free_list + kListHead;
   int32_t* marks = free_list + kListHead + n_blocks;
   const int64_t row_tokens = (int64_t)max_blocks << shift;
   const uint32_t most_tokens = (uint32_t)n_slots + 1, most_blocks = (uint32_t)n_blocks + 1;   // (more than there is: how much more does not matter)
-  uint32_t tokens = 0, blocks = 0;
-  if (tid == 0) s_take = 0;
-  for (int b0 = 0; b0 < n_b; b0 += kReserveThreads) {
-    const int b = b0 + tid;
-    int len = -1, n = 0;
-    if (b < n_b) { len = lens[b]; n = max(n_new[b], 0); }
+  // x[r] := sums over the requests up to each, cut to `most`
+  auto sums = [&](uint32_t (&x)[ROWS], uint32_t most) {
+#pragma unroll
+    for (int r = 1; r < ROWS; ++r) x[r] = min(x[r] + x[r - 1], most);
     uint32_t all;
-    const uint32_t end = min(scan_capped<kReserveThreads>(min((uint32_t)n, most_tokens), most_tokens, s_wave, all) + tokens, most_tokens);
-    tokens = min(tokens + all, most_tokens);
-    const bool fits = len >= 0 && (int64_t)len + n <= row_tokens && end <= (uint32_t)n_slots;
-    const int need = fits ? blocks_of(len + n, shift) - blocks_of(len, shift) : 0;
-    const uint32_t dealt = min(scan_capped<kReserveThreads>(min((uint32_t)need, most_blocks), most_blocks, s_wave, all) + blocks, most_blocks);
-    blocks = min(blocks + all, most_blocks);
-    const bool ok = fits && (need == 0 || dealt <= (uint32_t)n_free);
-    if (b < n_b) {
-      s_end[b] = (int)min(end, (uint32_t)n_slots);
-      s_dealt[b] = (int)dealt;
-      s_len[b] = ok ? len : -1;
-      if (ok && need > 0) atomicMax(&s_take, (int)dealt);
+    const uint32_t upto = scan_capped<kReserveThreads>(x[ROWS - 1], most, s_wave, all);
+    // (what is before this thread: the scan of the thread before, as cut sums cannot be taken apart)
+    uint32_t before = (uint32_t)__shfl_up((int)upto, 1);
+    if ((tid & 63) == 63) s_wave[tid >> 6] = upto;
+    __syncthreads();
+    if ((tid & 63) == 0) before = tid ? s_wave[(tid >> 6) - 1] : 0u;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) x[r] = min(x[r] + before, most);
+  };
+  uint32_t end[ROWS], dealt[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    fresh[r] = b0 + r < n_b ? max(fresh[r], 0) : 0;
+    end[r] = min((uint32_t)fresh[r], most_tokens);
+  }
+  sums(end, most_tokens);
+  bool fits[ROWS], needs[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    fits[r] = b0 + r < n_b && len[r] >= 0 && (int64_t)len[r] + fresh[r] <= row_tokens && end[r] <= (uint32_t)n_slots;
+    const int need = fits[r] ? blocks_of(len[r] + fresh[r], shift) - blocks_of(len[r], shift) : 0;
+    needs[r] = need > 0;
+    dealt[r] = min((uint32_t)need, most_blocks);
+  }
+  sums(dealt, most_blocks);
+  uint32_t dealt_here = 0;                 // up to the last request here that is served and needs any
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const bool ok = fits[r] && (!needs[r] || dealt[r] <= (uint32_t)n_free);
+    if (b0 + r < n_b) {
+      s_end[b0 + r] = (int)min(end[r], (uint32_t)n_slots);
+      s_dealt[b0 + r] = (int)dealt[r];
+      s_len[b0 + r] = ok ? len[r] : -1;
+      if (ok && needs[r]) dealt_here = dealt[r];
     }
   }
+  for (int w = 1; w < 64; w *= 2) dealt_here = max(dealt_here, (uint32_t)__shfl_xor((int)dealt_here, w));
+  if ((tid & 63) == 0) s_wave[tid >> 6] = dealt_here;
   __syncthreads();
-  const int total = s_end[n_b - 1], take = s_take;
-  for (int j = blockIdx.x * kReserveThreads + tid; j < n_slots; j += gridDim.x * kReserveThreads) {
-    int slot = -1;
-    if (j < total) {
-      const int b = owner_of(s_end, n_b, j), len = s_len[b];
-      if (len >= 0) {
-        const int t = len + (j - (b ? s_end[b - 1] : 0)), have = blocks_of(len, shift);
-        const int at = t >> shift;
-        const int blk = at < have ? table[(int64_t)b * max_blocks + at]
-                                  : stack[max(n_free - 1 - ((b ? s_dealt[b - 1] : 0) + (at - have)), 0)];
-        if ((unsigned)blk < (unsigned)n_blocks) slot = (blk << shift) + (t & ((1 << shift) - 1));
-      }
+  uint32_t take_all = 0;
+#pragma unroll
+  for (int w = 0; w < kReserveThreads / 64; ++w) take_all = max(take_all, s_wave[w]);
+  const int total = s_end[n_b - 1], take = (int)take_all, first = blockIdx.x * kReserveThreads * SLOTS;
+  const bool deals = first < take;         // (no request takes more blocks than tokens: block i goes with slot i)
+  int slot[SLOTS], owner[SLOTS], taker[SLOTS];
+#pragma unroll
+  for (int e = 0; e < SLOTS; ++e) slot[e] = first + e * kReserveThreads + tid;
+  owners_of(s_end, n_b, slot, owner);
+  if (deals) owners_of(s_dealt, n_b, slot, taker);
+  int off[SLOTS], blk[SLOTS], fresh_blk[SLOTS];                // a slot's offset in its block, -1: none
+  const int32_t* from[SLOTS];
+#pragma unroll
+  for (int e = 0; e < SLOTS; ++e) {
+    const int b = owner[e], had = s_len[b];
+    const int start = b ? s_end[b - 1] : 0, before = b ? s_dealt[b - 1] : 0;
+    off[e] = -1;
+    from[e] = stack;
+    if (slot[e] < total && had >= 0) {
+      const int t = had + (slot[e] - start), have = blocks_of(had, shift), at = t >> shift;
+      off[e] = t & ((1 << shift) - 1);
+      from[e] = at < have ? table + (int64_t)b * max_blocks + at : stack + max(n_free - 1 - (before + (at - have)), 0);
     }
-    slots[j] = slot;
-    if (j < take) {                        // (no request takes more blocks than tokens)
-      const int b = owner_of(s_dealt, n_b, j), k = j - (b ? s_dealt[b - 1] : 0);
-      const int blk = stack[n_free - 1 - j];
-      table[(int64_t)b * max_blocks + blocks_of(s_len[b], shift) + k] = blk;
-      if ((unsigned)blk < (unsigned)n_blocks) marks[blk] = kInUse;
+  }
+#pragma unroll
+  for (int e = 0; e < SLOTS; ++e) {
+    blk[e] = *from[e];
+    if (deals) fresh_blk[e] = stack[max(n_free - 1 - min(slot[e], take), 0)];
+  }
+#pragma unroll
+  for (int e = 0; e < SLOTS; ++e)
+    if (slot[e] < n_slots) slots[slot[e]] = off[e] >= 0 && (unsigned)blk[e] < (unsigned)n_blocks ? (blk[e] << shift) + off[e] : -1;
+  if (deals) {
+#pragma unroll
+    for (int e = 0; e < SLOTS; ++e) {
+      const int b = taker[e], k = slot[e] - (b ? s_dealt[b - 1] : 0);
+      if (slot[e] < take) {
+        table[(int64_t)b * max_blocks + blocks_of(s_len[b], shift) + k] = fresh_blk[e];
+        if ((unsigned)fresh_blk[e] < (unsigned)n_blocks) marks[fresh_blk[e]] = kInUse;
+      }
     }
   }
   if (blockIdx.x == 0) {
@@ -133,98 +204,116 @@ __global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
     __syncthreads();
   }
   for (int b = tid; b < n_b; b += kReserveThreads)
-    if (s_len[b] >= 0) lens[b] = s_len[b] + max(n_new[b], 0);
+    if (s_len[b] >= 0) lens[b] = s_len[b] + (s_end[b] - (b ? s_end[b - 1] : 0));   // (a request that is served has all of its slots)
   if (tid == 0) {
     free_list[0] = n_free - take;
     if (gridDim.x > 1) atomicExch(&free_list[1], 0);
   }
 }
 
-constexpr int kReturnThreads = 1024, kPerThread = 4;
+constexpr int kReturnThreads = 1024;
 
 // Blocks back onto the stack, in one workgroup: the order on the stack is that of the entries, the last one first, so that a
 // reservation that is taken back leaves the stack as it was.  An entry outside the pool, or one whose block is free already,
 // is passed over; of several entries with the same block one is taken: each leaves its place in the block's mark, and the
-// least one stays.
+// least one stays.  Whoever finds another place there (or a free block) says so, and only then are the marks read again.
 // TABLE: the entries of each row behind new_lens[b] tokens, which become -1; else the n_ids entries of `entries`.
-// dynamic LDS (TABLE): 4 bytes a row
-template <bool TABLE>
+// PER: entries a thread takes at a time, asked for together.  Bound by its trips to memory, four for the first 4096 entries (lengths,
+// entries, marks, stores) and three for every further ones.
+// dynamic LDS (TABLE): 8 bytes a row
+template <bool TABLE, int PER>
 __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* __restrict__ entries, int n_ids, int max_blocks,
                                                                       int n_b, int32_t* __restrict__ lens,
                                                                       const int32_t* __restrict__ new_lens,
                                                                       int32_t* __restrict__ free_list, int n_blocks, int shift) {
   extern __shared__ int32_t s_end[];       // entries up to each row, the last row first
+  int32_t* s_last = s_end + n_b;           // and the end of its entries
   __shared__ uint32_t s_wave[kReturnThreads / 64];
+  __shared__ int s_again;
   const int tid = threadIdx.x;
   int32_t* stack = free_list + kListHead;
   int32_t* marks = free_list + kListHead + n_blocks;
   int n_free = min(max(free_list[0], 0), n_blocks);
-  auto last_of = [&](int len) { return min(blocks_of(len, shift), max_blocks); };
   int total = n_ids;
+  if (tid == 0) s_again = 0;
   if (TABLE) {
     uint32_t sum = 0;
     for (int r0 = 0; r0 < n_b; r0 += kReturnThreads) {
       const int r = r0 + tid, b = n_b - 1 - r;
       uint32_t count = 0;
+      int last = 0;
       if (r < n_b) {
         const int len = lens[b], cut = new_lens[b];
-        if (cut >= 0 && cut < len) count = (uint32_t)max(last_of(len) - blocks_of(cut, shift), 0);
+        last = min(blocks_of(len, shift), max_blocks);
+        if (cut >= 0 && cut < len) {
+          count = (uint32_t)max(last - blocks_of(cut, shift), 0);
+          lens[b] = cut;                   // (this thread alone reads it)
+        }
       }
       uint32_t all;
       const uint32_t end = scan_capped<kReturnThreads>(count, 0x7fffffffu, s_wave, all) + sum;
-      if (r < n_b) s_end[r] = (int)end;
+      if (r < n_b) { s_end[r] = (int)end; s_last[r] = last; }
       sum += all;
     }
-    __syncthreads();
     total = (int)sum;
   }
-  for (int p0 = 0; p0 < total; p0 += kReturnThreads * kPerThread) {
-    const int first = p0 + tid * kPerThread;
-    int id[kPerThread];
+  __syncthreads();
+  for (int p0 = 0; p0 < total; p0 += kReturnThreads * PER) {
+    const int first = p0 + tid * PER;
+    int id[PER];
+    int64_t at[PER];
     int row = TABLE && first < total ? owner_of(s_end, n_b, first) : 0;
 #pragma unroll
-    for (int e = 0; e < kPerThread; ++e) {
+    for (int e = 0; e < PER; ++e) {
       const int p = first + e;
-      id[e] = -1;
+      at[e] = -1;
       if (p < total) {
-        int64_t at = n_ids - 1 - p;
         if (TABLE) {
           while (s_end[row] <= p) ++row;
-          const int b = n_b - 1 - row;
-          at = (int64_t)b * max_blocks + last_of(lens[b]) - 1 - (p - (row ? s_end[row - 1] : 0));
+          at[e] = (int64_t)(n_b - 1 - row) * max_blocks + s_last[row] - 1 - (p - (row ? s_end[row - 1] : 0));
+        } else {
+          at[e] = n_ids - 1 - p;
         }
-        id[e] = entries[at];
-        if (TABLE) entries[at] = -1;
-        if ((unsigned)id[e] >= (unsigned)n_blocks) id[e] = -1;
-        else atomicMin(&marks[id[e]], p);
       }
     }
-    __builtin_amdgcn_s_waitcnt(0);         // the marks have been lowered
-    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < PER; ++e) id[e] = at[e] >= 0 ? entries[at[e]] : -1;
+    bool again = false;
+    int found[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      if (TABLE && at[e] >= 0) entries[at[e]] = -1;
+      if ((unsigned)id[e] >= (unsigned)n_blocks) id[e] = -1;
+      found[e] = id[e] >= 0 ? atomicMin(&marks[id[e]], first + e) : kInUse;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) again |= found[e] != kInUse;
+    if (again) s_again = 1;
+    __syncthreads();                       // (every mark has been lowered: its old value is here)
+    if (s_again) {
+#pragma unroll
+      for (int e = 0; e < PER; ++e)
+        if (id[e] >= 0 && __hip_atomic_load(&marks[id[e]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != first + e) id[e] = -1;
+    }
     uint32_t mine = 0;
 #pragma unroll
-    for (int e = 0; e < kPerThread; ++e) {
-      if (id[e] >= 0 && __hip_atomic_load(&marks[id[e]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != first + e) id[e] = -1;
-      mine += id[e] >= 0;
-    }
+    for (int e = 0; e < PER; ++e) mine += id[e] >= 0;
     uint32_t all;
-    int to = n_free + (int)(scan_capped<kReturnThreads>(mine, 0x7fffffffu, s_wave, all) - mine);   // (behind its barrier all marks have been read)
+    int to = n_free + (int)(scan_capped<kReturnThreads>(mine, 0x7fffffffu, s_wave, all) - mine);   // (behind its barriers all marks have been read)
 #pragma unroll
-    for (int e = 0; e < kPerThread; ++e)
+    for (int e = 0; e < PER; ++e)
       if (id[e] >= 0) {
         if (to < n_blocks) stack[to] = id[e];
         ++to;
         __hip_atomic_store(&marks[id[e]], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     n_free = min(n_free + (int)all, n_blocks);
-    __builtin_amdgcn_s_waitcnt(0);         // (the next tile may hold the same blocks)
-    __syncthreads();
-  }
-  if (TABLE)
-    for (int b = tid; b < n_b; b += kReturnThreads) {
-      const int cut = new_lens[b];
-      if (cut >= 0 && cut < lens[b]) lens[b] = cut;
+    if (p0 + kReturnThreads * PER < total) {
+      if (tid == 0) s_again = 0;
+      __builtin_amdgcn_s_waitcnt(0);       // (the next ones may hold the same blocks)
+      __syncthreads();
     }
+  }
   if (tid == 0) free_list[0] = n_free;
 }
 
@@ -256,24 +345,36 @@ hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_
                                 int n_blocks, int shift, int32_t* slots, int n_slots, int32_t* starts, int32_t* granted,
                                 hipStream_t st) {
   ScopedTimer t("paged_reserve", st);
-  const int groups = n_slots > kSlotsPerGroup ? div_up(n_slots, kSlotsPerGroup) : 1;
-  hipLaunchKernelGGL(paged_reserve_kernel, dim3((unsigned)groups), dim3(kReserveThreads), (size_t)n_b * 12, st, table, lens, n_new,
-                     free_list, n_b, max_blocks, n_blocks, shift, slots, n_slots, starts, granted);
+  const bool few = n_slots <= 32 * kReserveThreads;    // (more workgroups than that have more to do with counting themselves in)
+  const int groups = n_slots > 0 ? div_up(n_slots, kReserveThreads * (few ? 1 : 4)) : 1;
+#define CKV_RESERVE(rows, slots_each)                                                                                      \
+  hipLaunchKernelGGL((paged_reserve_kernel<rows, slots_each>), dim3((unsigned)groups), dim3(kReserveThreads), (size_t)n_b * 12, st, table, \
+                     lens, n_new, free_list, n_b, max_blocks, n_blocks, shift, slots, n_slots, starts, granted)
+#define CKV_RESERVE_ROWS(slots_each)                                 \
+  do {                                                               \
+    if (n_b <= kReserveThreads) CKV_RESERVE(1, slots_each);          \
+    else if (n_b <= 4 * kReserveThreads) CKV_RESERVE(4, slots_each); \
+    else CKV_RESERVE(16, slots_each);                                \
+  } while (0)
+  if (few) CKV_RESERVE_ROWS(1);
+  else CKV_RESERVE_ROWS(4);
+#undef CKV_RESERVE_ROWS
+#undef CKV_RESERVE
   return hipGetLastError();
 }
 
 hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int n_b, int max_blocks,
                              int n_blocks, int shift, hipStream_t st) {
   ScopedTimer t("paged_trim", st);
-  hipLaunchKernelGGL(paged_return_kernel<true>, dim3(1), dim3(kReturnThreads), (size_t)n_b * 4, st, table, 0, max_blocks, n_b, lens,
-                     new_lens, free_list, n_blocks, shift);
+  hipLaunchKernelGGL((paged_return_kernel<true, 4>), dim3(1), dim3(kReturnThreads), (size_t)n_b * 8, st, table, 0, max_blocks, n_b,
+                     lens, new_lens, free_list, n_blocks, shift);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int n_blocks, hipStream_t st) {
   if (n == 0) return hipSuccess;
   ScopedTimer t("paged_free", st);
-  hipLaunchKernelGGL(paged_return_kernel<false>, dim3(1), dim3(kReturnThreads), 0, st, const_cast<int32_t*>(ids), n, 0, 0,
+  hipLaunchKernelGGL((paged_return_kernel<false, 4>), dim3(1), dim3(kReturnThreads), 0, st, const_cast<int32_t*>(ids), n, 0, 0,
                      static_cast<int32_t*>(nullptr), static_cast<const int32_t*>(nullptr), free_list, n_blocks, 0);
   return hipGetLastError();
 }
