@@ -42,18 +42,7 @@ __device__ __forceinline__ uint32_t scan_capped(uint32_t x, uint32_t most, uint3
   return min(x + before, most);
 }
 
-// first i in [0, n) with end[i] > x (end does not fall; there is one)
-__device__ __forceinline__ int owner_of(const int32_t* end, int n, int x) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (end[mid] > x) hi = mid;
-    else lo = mid + 1;
-  }
-  return lo;
-}
-
-// the same for E values at once (n - 1 where there is none): their reads of LDS go together
+// at[e] = first i in [0, n) with end[i] > x[e], n - 1 where there is none (end does not fall): the searches' reads of LDS go together
 template <int E>
 __device__ __forceinline__ void owners_of(const int32_t* end, int n, const int (&x)[E], int (&at)[E]) {
 #pragma unroll
@@ -218,10 +207,12 @@ constexpr int kReturnThreads = 1024;
 // is passed over; of several entries with the same block one is taken: each leaves its place in the block's mark, and the
 // least one stays.  Whoever finds another place there (or a free block) says so, and only then are the marks read again.
 // TABLE: the entries of each row behind new_lens[b] tokens, which become -1; else the n_ids entries of `entries`.
-// PER: entries a thread takes at a time, asked for together.  Bound by its trips to memory, four for the first 4096 entries (lengths,
-// entries, marks, stores) and three for every further ones.
+// A thread takes kPer entries at a time, neighbours neighbouring ones, and asks for them together; the entries before its own
+// are counted by ballots, one word for 64 of them.  (Four in a row a thread, rows sought one after the other: 33 rows of
+// 4200 entries 21 us, 1000 rows of 160 9.5.)
 // dynamic LDS (TABLE): 8 bytes a row
-template <bool TABLE, int PER>
+constexpr int kPer = 64 / (kReturnThreads / 64);
+template <bool TABLE>
 __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* __restrict__ entries, int n_ids, int max_blocks,
                                                                       int n_b, int32_t* __restrict__ lens,
                                                                       const int32_t* __restrict__ new_lens,
@@ -229,7 +220,7 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
   extern __shared__ int32_t s_end[];       // entries up to each row, the last row first
   int32_t* s_last = s_end + n_b;           // and the end of its entries
   __shared__ uint32_t s_wave[kReturnThreads / 64];
-  __shared__ int s_again;
+  __shared__ int s_again, s_count[64], s_total;
   const int tid = threadIdx.x;
   int32_t* stack = free_list + kListHead;
   int32_t* marks = free_list + kListHead + n_blocks;
@@ -258,57 +249,61 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
     total = (int)sum;
   }
   __syncthreads();
-  for (int p0 = 0; p0 < total; p0 += kReturnThreads * PER) {
-    const int first = p0 + tid * PER;
-    int id[PER];
-    int64_t at[PER];
-    int row = TABLE && first < total ? owner_of(s_end, n_b, first) : 0;
+  const int lane = tid & 63, wave = tid >> 6;
+  for (int p0 = 0; p0 < total; p0 += kReturnThreads * kPer) {
+    int p[kPer], row[kPer], id[kPer], found[kPer];
+    int64_t at[kPer];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const int p = first + e;
+    for (int e = 0; e < kPer; ++e) p[e] = p0 + e * kReturnThreads + tid;
+    if (TABLE) owners_of(s_end, n_b, p, row);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
       at[e] = -1;
-      if (p < total) {
-        if (TABLE) {
-          while (s_end[row] <= p) ++row;
-          at[e] = (int64_t)(n_b - 1 - row) * max_blocks + s_last[row] - 1 - (p - (row ? s_end[row - 1] : 0));
-        } else {
-          at[e] = n_ids - 1 - p;
-        }
+      if (p[e] < total) {
+        if (TABLE) at[e] = (int64_t)(n_b - 1 - row[e]) * max_blocks + s_last[row[e]] - 1 - (p[e] - (row[e] ? s_end[row[e] - 1] : 0));
+        else at[e] = n_ids - 1 - p[e];
       }
     }
 #pragma unroll
-    for (int e = 0; e < PER; ++e) id[e] = at[e] >= 0 ? entries[at[e]] : -1;
-    bool again = false;
-    int found[PER];
+    for (int e = 0; e < kPer; ++e) id[e] = at[e] >= 0 ? entries[at[e]] : -1;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      if (TABLE && at[e] >= 0) entries[at[e]] = -1;
+    for (int e = 0; e < kPer; ++e) {
       if ((unsigned)id[e] >= (unsigned)n_blocks) id[e] = -1;
-      found[e] = id[e] >= 0 ? atomicMin(&marks[id[e]], first + e) : kInUse;
+      found[e] = id[e] >= 0 ? atomicMin(&marks[id[e]], p[e]) : kInUse;
+      if (TABLE && at[e] >= 0) entries[at[e]] = -1;
     }
+    bool again = false;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) again |= found[e] != kInUse;
+    for (int e = 0; e < kPer; ++e) again |= found[e] != kInUse;
     if (again) s_again = 1;
     __syncthreads();                       // (every mark has been lowered: its old value is here)
     if (s_again) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e)
-        if (id[e] >= 0 && __hip_atomic_load(&marks[id[e]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != first + e) id[e] = -1;
+      for (int e = 0; e < kPer; ++e)
+        if (id[e] >= 0 && __hip_atomic_load(&marks[id[e]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != p[e]) id[e] = -1;
     }
-    uint32_t mine = 0;
+    uint64_t taken[kPer];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) mine += id[e] >= 0;
-    uint32_t all;
-    int to = n_free + (int)(scan_capped<kReturnThreads>(mine, 0x7fffffffu, s_wave, all) - mine);   // (behind its barriers all marks have been read)
+    for (int e = 0; e < kPer; ++e) {
+      taken[e] = __ballot(id[e] >= 0);
+      if (lane == 0) s_count[e * (kReturnThreads / 64) + wave] = (int)__popcll(taken[e]);
+    }
+    __syncthreads();                       // (and all marks have been read)
+    if (wave == 0) {
+      const int upto = (int)wave_inclusive_scan((uint32_t)s_count[lane]);
+      s_count[lane] = upto - s_count[lane];
+      if (lane == 63) s_total = upto;
+    }
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < PER; ++e)
+    for (int e = 0; e < kPer; ++e)
       if (id[e] >= 0) {
+        const int to = n_free + s_count[e * (kReturnThreads / 64) + wave] + (int)__popcll(taken[e] & ((1ull << lane) - 1));
         if (to < n_blocks) stack[to] = id[e];
-        ++to;
         __hip_atomic_store(&marks[id[e]], -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
-    n_free = min(n_free + (int)all, n_blocks);
-    if (p0 + kReturnThreads * PER < total) {
+    n_free = min(n_free + s_total, n_blocks);
+    if (p0 + kReturnThreads * kPer < total) {
       if (tid == 0) s_again = 0;
       __builtin_amdgcn_s_waitcnt(0);       // (the next ones may hold the same blocks)
       __syncthreads();
@@ -366,7 +361,7 @@ hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_
 hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int n_b, int max_blocks,
                              int n_blocks, int shift, hipStream_t st) {
   ScopedTimer t("paged_trim", st);
-  hipLaunchKernelGGL((paged_return_kernel<true, 4>), dim3(1), dim3(kReturnThreads), (size_t)n_b * 8, st, table, 0, max_blocks, n_b,
+  hipLaunchKernelGGL((paged_return_kernel<true>), dim3(1), dim3(kReturnThreads), (size_t)n_b * 8, st, table, 0, max_blocks, n_b,
                      lens, new_lens, free_list, n_blocks, shift);
   return hipGetLastError();
 }
@@ -374,7 +369,7 @@ hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_l
 hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int n_blocks, hipStream_t st) {
   if (n == 0) return hipSuccess;
   ScopedTimer t("paged_free", st);
-  hipLaunchKernelGGL((paged_return_kernel<false, 4>), dim3(1), dim3(kReturnThreads), 0, st, const_cast<int32_t*>(ids), n, 0, 0,
+  hipLaunchKernelGGL((paged_return_kernel<false>), dim3(1), dim3(kReturnThreads), 0, st, const_cast<int32_t*>(ids), n, 0, 0,
                      static_cast<int32_t*>(nullptr), static_cast<const int32_t*>(nullptr), free_list, n_blocks, 0);
   return hipGetLastError();
 }
