@@ -65,9 +65,9 @@ constexpr int kReserveThreads = 256;
 // already or in one that this call deals, the i-th block dealt being the i-th from the stack's top.  Nothing that one workgroup
 // writes is read by another: lengths and the number of free blocks change when the last one has read them.
 //
-// What bounds it: a chain of trips to memory (lengths; entry or stack; store), for 64 requests of one token each the whole of its 3.5 us.
-// So a thread takes ROWS requests in a row (1000 requests, one and a pair of sums at a time: 12.3 us) and asks for the
-// entries of its slots together (135000 slots, one after the other: 8.8 us).
+// What bounds it: a chain of trips to memory (lengths; entry or stack; store) and of reads of LDS, for 64 requests of one token
+// each the whole of its 4.3 us.  So a thread takes ROWS requests in a row and searches for the owners of its SLOTS slots
+// together (1000 requests, 256 at a time, slot by slot: 12.1 us, now 7.6; 33 prompts of 135000 slots 8.8, now 8.1).
 // dynamic LDS: 12 bytes a request
 template <int ROWS, int SLOTS>   // a thread's requests and slots
 __global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
@@ -208,8 +208,9 @@ constexpr int kReturnThreads = 1024;
 // least one stays.  Whoever finds another place there (or a free block) says so, and only then are the marks read again.
 // TABLE: the entries of each row behind new_lens[b] tokens, which become -1; else the n_ids entries of `entries`.
 // A thread takes kPer entries at a time, neighbours neighbouring ones, and asks for them together; the entries before its own
-// are counted by ballots, one word for 64 of them.  (Four in a row a thread, rows sought one after the other: 33 rows of
-// 4200 entries 21 us, 1000 rows of 160 9.5.)
+// are counted by ballots, one word for 64 of them.  Bound by its trips to memory (lengths, entries, marks, stores: 4.7 us for 64 rows
+// that give back four blocks) and, for thousands of entries, by one CU's scattered ones (33 rows of 4200 entries 19 us).
+// With four entries in a row a thread and their rows sought one after the other 7.4 and 21.
 // dynamic LDS (TABLE): 8 bytes a row
 constexpr int kPer = 64 / (kReturnThreads / 64);
 template <bool TABLE>
@@ -313,7 +314,8 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
 }
 
 // Rows of k and v [n, heads, dim] into the pool by their slots (block * block_size + offset), degree 1; a slot outside the
-// pool is passed over.  Bound by its bytes: a thread takes 16-byte pieces, consecutive ones of a row, of both tensors.
+// pool is passed over.  A thread takes 16-byte pieces of both tensors, consecutive threads consecutive ones of a row.  Bound by
+// its bytes: 50021 rows of 8 heads of 128 bf16, 411 MB read and written, take 84 us, 4.9 TB/s (a large copy: 5.2).
 constexpr int kWriteThreads = 256, kWritePieces = 4;
 __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
     const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, int64_t row_stride, int64_t head_stride,

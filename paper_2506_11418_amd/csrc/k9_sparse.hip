@@ -16,7 +16,8 @@ namespace {
 // negative ones are turned over: five instructions for two bf16 and their place in both bounds, where fp32 comparisons that
 // keep NaN take 18.  A NaN lies beyond the infinity of its sign, so that it ends up in one of the two bounds; both become NaN then.
 //
-// What bounds it: reads (402 MB of keys and 13 of degrees in 122 us with fp32 comparisons, degrees waited for before keys).
+// What bounds it: reads.  402 MB of keys, 13 of degrees and 50 of bounds (8 sequences of up to 32768 tokens, 8 heads) take 86 us, 5.4 TB/s;
+// with fp32 comparisons and the degrees waited for before the keys 122.
 constexpr int kBoundsThreads = 256, kBoundsWaves = kBoundsThreads / 64;
 template <typename T> struct Ordered;
 template <> struct Ordered<__bf16> {     // two a word
@@ -136,9 +137,13 @@ __device__ __forceinline__ uint32_t rank_of(double dot, double scale, int mass) 
 // and infinity the score is not finite either way.)  A 16-byte piece of a row goes to lane block + 16 (piece % 4), and the
 // queries wait in fp32, as they are in 64 bits, in the order of the pieces.
 //
-// What bounds it: 16 cycles of the matrix unit and 12 of the vector unit (two conversions, one unpacking) for 64 bounds, 128
-// bytes in bf16: 16 TB/s over the chip, so that memory decides.  One wave a block with vector arithmetic and sums over the lanes
-// took 165 us for 100 MB.
+// Why this instruction: the sums have to be in 64 bits (see rank_of), and it takes 16 cycles for 64 bounds and four heads where vector
+// arithmetic takes 8 for each head, and leaves four lanes to compare instead of sums over sixteen (one wave a block with vector
+// arithmetic: 100 MB 165 us, now 29).  The 16x16x4 form takes 64 cycles for sixteen columns, of which four or eight are heads.
+//
+// What bounds it: 268 MB (one sequence of 65536 blocks, 8 heads of 4) take 58 us, 4.6 TB/s.  Matrix unit busy 27 %, vector unit 38 % of the
+// cycles (counted; they share the 64-bit arithmetic); the rest are waits for rows of 512 bytes in no order.  Neither
+// more nor fewer waves help (two workgroups a CU 63 us, four 59, six 61), nor the queries held in 64 bits (60).
 template <typename T, int D, int G>
 struct ScoreTile {
   static constexpr int E = 16 / sizeof(T);                 // bounds in a piece
@@ -274,7 +279,8 @@ __global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged
 //
 // One CU takes half a microsecond for every instruction that 65536 keys need, so that long rows are cut into segments: a
 // workgroup each finds the keys of its segment that can be among the largest, and one more takes the cut among those
-// (65536 blocks of 8 heads, 256 of them: 49 us in one step).
+// (65536 blocks of 8 heads, 256 of them: 49 us in one step, 20 in two launches).  Short rows are bound by the chain of
+// steps between barriers: 6.4 us for 129 blocks of 8 heads, 7.0 for 2048 of 128.
 enum class Step { WHOLE, SEGMENT, JOIN };
 constexpr int kBins = 2048;
 template <int THREADS>
@@ -367,7 +373,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
     }
   };
   // the range of the keys
-  if (tid == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0u; s_end = 0; }
+  if (tid == 0) { s_range[0] = 0xffffffffu; s_range[1] = 0u; s_end = 0; s_found[0] = s_found[1] = s_found[2] = 0; }
   __syncthreads();
   {
     uint32_t least_key = 0xffffffffu, most_key = 0u;         // (of the key below: 0 becomes the largest)
@@ -386,7 +392,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
   bool whole = false;                            // all of them
   const bool none = want == 0;
   int left = want;                               // to be taken in [from, to], counted from the top
-  while (left > 0) {
+  for (int round = 0; left > 0 && round < 3; ++round) {       // (three digits of 11 bits: from == to then, whatever the keys)
     const uint32_t width = to - from;
     const int shift = width < kBins ? 0 : 32 - __clz(width) - 11;
     for (int i = tid; i < kBins; i += THREADS) s_hist[i] = 0;
@@ -451,6 +457,7 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
     for (int j = 0; j < KEYS; ++j)
       if (taken(j)) {
         const int i = span * SPAN + j * THREADS + tid, to_place = place_of(j);
+        if (to_place >= want) continue;          // (never, unless another call writes this one's scratch)
         if constexpr (STEP == Step::SEGMENT) {
           uint32_t* kept = c.kept + (bh * c.segments * 2 + blockIdx.z) * c.most + to_place;
           kept[0] = x[j];
@@ -478,7 +485,8 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
 
 template <typename T, int D, int G>
 hipError_t launch_scores(const SelectCall& c) {
-  // waves that run at once, as long as each has a tile, and whole heads
+  // waves that run at once, three workgroups a CU, as long as each has a tile; and whole heads, so that the rows of a block that
+  // lie side by side are read together (a head a workgroup: 268 MB 67 us)
   const int tiles = div_up(c.key_stride, 16), fit = div_up(3 * kScoreWaves * cu_count(), c.n_b * c.heads);
   const int waves = (tiles < fit ? tiles : fit) * c.heads;
   hipLaunchKernelGGL((paged_score_kernel<T, D, G>), dim3((unsigned)div_up(waves, kScoreWaves), (unsigned)c.n_b),

@@ -1,5 +1,7 @@
 """What the table, slot and selection calls refuse, found on the host before any launch; and their sizes.  No GPU needed."""
 import ctypes as C
+import re
+import struct
 
 import pytest
 import torch
@@ -150,3 +152,70 @@ def test_python_refuses_what_does_not_fit_together():
         ckv.paged_free(i32(3).long(), free)
     with pytest.raises(ValueError):
         ckv.paged_free_list(0)
+
+
+class _OnGpu(torch.Tensor):
+    """A host tensor that says it lives on the GPU; nothing here follows its pointer."""
+    is_cuda = property(lambda self: True)
+    get_device = lambda self: 0
+
+
+def _made_calls():
+    t = lambda *s, dtype=torch.int32: torch.zeros(s, dtype=dtype).as_subclass(_OnGpu)
+    h = lambda *s: t(*s, dtype=torch.bfloat16)
+    table, lens, free, ws = t(2, 4), t(2), t(4 + 2 * 6), t(1 << 16, dtype=torch.uint8)
+    pool, bounds, mass, q, sel, sel_lens = h(6, 2, 16, 64), h(6, 2, 2, 64), t(6, 2), h(2, 8, 64), t(2, 2, 3), t(2, 2)
+    return {
+        "ckv_paged_reserve": lambda: ckv.paged_reserve(table, lens, t(2), free, 16, 5, out=(t(5), t(3), t(2))),
+        "ckv_paged_trim": lambda: ckv.paged_trim(table, lens, t(2), free, 16),
+        "ckv_paged_write": lambda: ckv.paged_write(h(5, 2, 64), h(5, 2, 64), t(5), pool, pool, t(6, 2, 16)),
+        "ckv_paged_bounds": lambda: ckv.paged_bounds(pool, None, table, lens, 9, out=(bounds, mass)),
+        "ckv_paged_select": lambda: ckv.paged_select(q, bounds, mass, table, lens, 64, 3, 16, out=(sel, sel_lens), workspace=ws),
+        "ckv_paged_sparse_decode_attn": lambda: ckv.paged_sparse_decode_attn(q, pool, pool, None, sel, sel_lens, out=q, workspace=ws),
+    }
+
+
+@pytest.mark.parametrize("name", list(_made_calls()))
+@pytest.mark.parametrize("status", [-6, -2, None])
+def test_a_call_is_made_once_by_either_route(monkeypatch, name, status):
+    """A status of the binding ends the call; None goes on to ctypes, which makes it once."""
+    class Answer:
+        def __getattr__(self, _):
+            return lambda *a: status
+
+    class Calls:
+        made, real = [], ckv.lib()
+
+        def __getattr__(self, n):
+            if n == "ckv_strerror":
+                return self.real.ckv_strerror
+            return lambda *a: self.made.append(n) or 0
+    calls = Calls()
+    Calls.made = []
+    monkeypatch.setattr(ckv, "lib", lambda: calls)
+    monkeypatch.setattr(ckv, "_here", lambda: (0, 0))
+    monkeypatch.setattr(ckv, "_stream", lambda: None)
+    monkeypatch.setattr(ckv, "_native", Answer())
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    if status is None:
+        _made_calls()[name]()
+        assert Calls.made == [name]
+    else:
+        with pytest.raises(ckv.CkvError) as e:
+            _made_calls()[name]()
+        assert e.value.status == status and str(e.value).startswith(name + ":") and not Calls.made
+
+
+def test_registers_of_the_paged_kernels():
+    """No scratch, and the waves a SIMD that the launches count on."""
+    pytest.importorskip("msgpack")
+    from test_kernel_resources import LIB, _instances, _metadata
+    data, found = open(LIB, "rb").read(), {}
+    for at in (m.start() for m in re.finditer(b"\x7fELF", data)):
+        if struct.unpack_from("<H", data, at + 18)[0] == 224:       # EM_AMDGPU
+            found.update({k[".name"]: (k[".vgpr_count"], k[".private_segment_fixed_size"]) for k in _metadata(data[at:])})
+    mine = {k: v for k, v in found.items() if re.search("N_1[0-9]+paged_(score|select|bounds|reserve|return|write)_kernel", k)}
+    assert len(mine) > 30 and all(scratch == 0 for _, scratch in mine.values())
+    scores = _instances(found, "paged_score_kernel")
+    assert len(scores) == 5 * 4 and all(use[0] <= 168 for k, use in scores.items() if k[0] == "DF16b" and (k[1], k[2]) != ("128", "8"))
