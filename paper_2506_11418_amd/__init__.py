@@ -4,7 +4,7 @@ Only argument marshalling happens here: torch tensors provide device memory and 
 stream; every step of the path runs in the library's kernels.  There is no CPU fallback: if the
 shared library has not been built, or a call fails, an exception is raised.
 
-The calls of a decode step and compress() are marshalled by csrc/binding.cpp when outputs and workspace are
+The calls of a decode step, paged and sparse ones too, and compress() are marshalled by csrc/binding.cpp when outputs and workspace are
 passed in and everything is well-formed (one layer's step over a 515-token cache, append and attention, two
 launches: 12.1 us, 27.6 with ctypes; compress() of 1024 tokens 3.9 us on the caller's side, 15).  What it does not
 take (None) goes on to the ctypes route below, which makes the call or reports it.  A status means that the call has

@@ -315,9 +315,9 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
 
 // Rows of k and v [n, heads, dim] into the pool by their slots (block * block_size + offset), degree 1; a slot outside the
 // pool is passed over.  A thread takes 16-byte pieces of both tensors, consecutive threads consecutive ones of a row, and asks for
-// eight before it stores one.  Bound by its bytes: 50021 rows of 8 heads of 128 bf16, 411 MB read and written, take 64 us,
-// 6.4 TB/s.  Rows are read once and not kept, pages are (rows read like others 82 us, pages not kept 79, one piece of each tensor
-// at a time 84).
+// eight before it stores one.  Bound by its bytes: 50021 rows of 8 heads of 128 bf16, 411 MB read and written, take 80 us on inputs
+// that are new each time, 5.2 TB/s, what a large copy reaches (stores that keep the pages in the caches 84; the same inputs
+// over and over, half of them still there, 64).
 constexpr int kWriteThreads = 256, kWritePieces = 4;
 __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
     const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, int64_t row_stride, int64_t head_stride,
@@ -343,8 +343,8 @@ __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
     for (int u = 0; u < kWritePieces; ++u) {
       if (e0 + u * kWriteThreads >= total || slot[u] < 0 || (slot[u] >> shift) >= n_blocks) continue;
       const int64_t row = ((((int64_t)(slot[u] >> shift) * heads + h[u]) << shift) + (slot[u] & ((1 << shift) - 1)));
-      *reinterpret_cast<uint4*>(K_pool + (row * pieces_per_row + piece[u]) * 16) = a[u];
-      *reinterpret_cast<uint4*>(V_pool + (row * pieces_per_row + piece[u]) * 16) = c[u];
+      stg16_stream(K_pool + (row * pieces_per_row + piece[u]) * 16, a[u]);
+      stg16_stream(V_pool + (row * pieces_per_row + piece[u]) * 16, c[u]);
       if (piece[u] == 0 && deg_pool) deg_pool[row] = 1;
     }
   }

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged
   };
   auto id_of = [&](int i0) { return table[min(i0 + row, hi - 1)]; };
   // whole rows, consecutive lanes consecutive pieces (lane block + 16 piece straight from memory takes a row of cache tags for every four
-  // lanes: 268 MB 80 us, so 69), read once and not kept: the caches have better use for their room (with ordinary loads 166 us)
+  // lanes: 268 MB 80 us, so 69), read once and not kept (with ordinary loads a whole pass of 88 us takes 201)
   auto issue = [&](Tile& t, int blk) {
     const bool in = (unsigned)blk < (unsigned)paged.n_blocks;
     const int slab = (in ? blk : 0) * heads + h;
