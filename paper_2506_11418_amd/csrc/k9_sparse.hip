@@ -185,7 +185,10 @@ __global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged
       const int at = (4 * j + k) * E;
       const Piece16 p = *reinterpret_cast<const Piece16*>(q + (((int64_t)b * heads + h) * G + (s * 4 + (lane & 3)) % G) * D + at % D);
 #pragma unroll
-      for (int e = 0; e < E; ++e) qv[s][j][e] = at < D ? fminf((float)p.x[e], 0.f) : fmaxf((float)p.x[e], 0.f);
+      for (int e = 0; e < E; ++e) {
+        const float x = (float)p.x[e];
+        qv[s][j][e] = (at < D ? x > 0.f : x < 0.f) ? 0.f : x;   // (a NaN stays one in both parts; fminf and fmaxf would drop it)
+      }
     }
 
   unsigned char* tile = s_tile + wave * S::BYTES;
