@@ -869,11 +869,19 @@ int check_tables(int32_t batch, int32_t max_blocks, int32_t n_blocks, int32_t bl
 }
 // whether no two of these overlap (NULL and empty ones do not)
 struct Span { const void* p; size_t bytes; };
+bool meet(const Span& a, const Span& b) { return a.p && b.p && a.bytes && b.bytes && ckv::overlaps(a.p, a.bytes, b.p, b.bytes); }
 bool apart(std::initializer_list<Span> all) {
   for (const Span& a : all)
     for (const Span& b : all)
-      if (&a != &b && a.p && b.p && a.bytes && b.bytes && ckv::overlaps(a.p, a.bytes, b.p, b.bytes)) return false;
+      if (&a != &b && meet(a, b)) return false;
   return true;
+}
+// whether nothing that is written overlaps what is read, or anything else that is written
+bool writes_apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span& w : written)
+    for (const Span& r : read)
+      if (meet(w, r)) return false;
+  return apart(written);
 }
 bool misaligned4(std::initializer_list<const void*> ps) {
   for (const void* p : ps)
@@ -935,8 +943,8 @@ int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t he
     return CKV_EALIGN;
   if (misaligned4({slots, deg_pool})) return CKV_EALIGN;
   const size_t in = (size_t)((int64_t)(n - 1) * row_stride + (int64_t)(pl->heads - 1) * head_stride + pl->dim) * e;   // (k and v may share rows)
-  const size_t pool = (size_t)pl->n_blocks * pl->heads * pl->block_size * pl->dim * e;
-  if (!apart({{k, in}, {K_pool, pool}, {V_pool, pool}}) || !apart({{v, in}, {K_pool, pool}, {V_pool, pool}})) return CKV_EINVAL;
+  const size_t rows = (size_t)pl->n_blocks * pl->heads * pl->block_size, pool = rows * pl->dim * e;
+  if (!writes_apart({{K_pool, pool}, {V_pool, pool}, {deg_pool, rows * 4}}, {{k, in}, {v, in}, {slots, (size_t)n * 4}})) return CKV_EINVAL;
   return ckv::hip_status(ckv::launch_paged_write(k, v, row_stride * e, head_stride * e, slots, n, K_pool, V_pool, deg_pool, pl->heads,
                                                  pl->dim * e, shift, pl->n_blocks, static_cast<hipStream_t>(hip_stream)));
 }
@@ -978,8 +986,11 @@ int ckv_paged_bounds(const void* K_pool, const int32_t* deg_pool, const int32_t*
   if (max_new <= 0) return CKV_ESHAPE;
   if (!K_pool || !block_table || !lens || !bounds || !mass) return CKV_EINVAL;
   if (((uintptr_t)K_pool | (uintptr_t)bounds) % 16 || misaligned4({deg_pool, block_table, lens, since, mass})) return CKV_EALIGN;
-  const size_t e = ckv::elem_bytes(pl->dtype), pairs = (size_t)pl->n_blocks * pl->heads;
-  if (ckv::overlaps(K_pool, pairs * pl->block_size * pl->dim * e, bounds, pairs * 2 * pl->dim * e)) return CKV_EINVAL;
+  const size_t row = (size_t)pl->dim * ckv::elem_bytes(pl->dtype), pairs = (size_t)pl->n_blocks * pl->heads, n = (size_t)pl->batch * 4;
+  if (!writes_apart({{bounds, pairs * 2 * row}, {mass, pairs * 4}},
+                    {{K_pool, pairs * pl->block_size * row}, {deg_pool, pairs * pl->block_size * 4}, {block_table, n * pl->max_blocks}, {lens, n},
+                     {since, n}}))
+    return CKV_EINVAL;
   return ckv::hip_status(ckv::launch_paged_bounds(K_pool, deg_pool, pl->dtype, ckv::PagedView{block_table, pl->max_blocks, shift, pl->n_blocks},
                                                   lens, since, max_new, pl->batch, pl->heads, pl->dim, bounds, mass,
                                                   static_cast<hipStream_t>(hip_stream)));
@@ -1012,6 +1023,10 @@ int ckv_paged_select(const void* q, int32_t q_heads, const void* bounds, const i
   if (workspace_bytes < need) return CKV_EWORKSPACE;
   const int G = q_heads / pl->heads;
   if (G != 1 && G != 2 && G != 4 && G != 8) return CKV_EUNSUPPORTED;
+  const size_t row = (size_t)pl->dim * ckv::elem_bytes(pl->dtype), pairs = (size_t)pl->n_blocks * pl->heads, n = (size_t)pl->batch * 4;
+  if (!writes_apart({{sel, n * pl->heads * n_select}, {sel_lens, n * pl->heads}, {workspace, need}},
+                    {{q, (size_t)pl->batch * q_heads * row}, {bounds, pairs * 2 * row}, {mass, pairs * 4}, {block_table, n * pl->max_blocks}, {lens, n}}))
+    return CKV_EINVAL;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)pl->dim);
   int shift;
   check_paged(pl, &shift);
@@ -1051,6 +1066,11 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
   if (st != CKV_OK) return st;
   ckv_paged_layout sl;
   sparse_layout(pl, n_select, &sl);
+  const size_t row = (size_t)pl->dim * ckv::elem_bytes(pl->dtype), rows = (size_t)pl->n_blocks * pl->heads * pl->block_size;
+  const size_t pairs = (size_t)sl.batch * 4, heads = (size_t)pl->batch * q_heads;
+  if (!writes_apart({{o, heads * pl->dim * ckv::elem_bytes(o_dtype)}, {workspace, workspace_bytes < reserve ? workspace_bytes : reserve}},
+                    {{q, heads * row}, {K_pool, rows * row}, {V_pool, rows * row}, {deg_pool, rows * 4}, {sel, pairs * n_select}, {sel_lens, pairs}}))
+    return CKV_EINVAL;
   return ckv_paged_decode_attn(q, q_heads / pl->heads, K_pool, V_pool, deg_pool, sel, sel_lens, &sl, n_select * pl->block_size, scale,
                                o, o_dtype, workspace, workspace_bytes, hip_stream);
 }
