@@ -530,6 +530,13 @@ def _ints(what: str, t: torch.Tensor, *shape) -> None:
         raise ValueError(f"{what} must be a contiguous int32 [{', '.join('any' if n is None else str(n) for n in shape)}] tensor")
 
 
+def _i32(**numbers) -> None:
+    """Numbers that the library takes as int32: ctypes would cut larger ones to their lower bits without a word."""
+    for what, n in numbers.items():
+        if not -2**31 <= n < 2**31:
+            raise ValueError(f"{what} = {n} does not fit 32 bits")
+
+
 def _pool_blocks(free_list: torch.Tensor) -> int:
     _ints("free_list", free_list, None)
     if free_list.numel() < 6 or free_list.numel() % 2:
@@ -552,6 +559,7 @@ def paged_reserve(block_table, lens, n_new, free_list, block_size: int, n_slots:
     n_blocks = _pool_blocks(free_list)
     _ints("lens", lens, B)
     _ints("n_new", n_new, B)
+    _i32(block_size=block_size, n_slots=n_slots)
     if n_slots < 0:
         raise ValueError("n_slots must not be negative")
     if out is None:
@@ -582,6 +590,7 @@ def paged_trim(block_table, lens, new_lens, free_list, block_size: int) -> None:
     n_blocks = _pool_blocks(free_list)
     _ints("lens", lens, B)
     _ints("new_lens", new_lens, B)
+    _i32(block_size=block_size)
     _on_this_gpu(block_table, lens, new_lens, free_list)
     st = lib().ckv_paged_trim(_ptr(block_table), _ptr(lens), _ptr(new_lens), _ptr(free_list), B, width, n_blocks, block_size,
                               _stream())
@@ -595,6 +604,7 @@ def paged_free(ids, free_list) -> None:
     n_blocks = _pool_blocks(free_list)
     if ids.dtype != torch.int32 or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous int32 tensor")
+    _i32(ids=ids.numel())
     _on_this_gpu(ids, free_list)
     st = lib().ckv_paged_free(_ptr(ids), ids.numel(), _ptr(free_list), n_blocks, _stream())
     if st != 0:
@@ -653,6 +663,7 @@ def paged_bounds(K_pool, deg_pool, block_table, lens, max_new: int, since=None, 
     _ints("lens", lens, pl.batch)
     if since is not None:
         _ints("since", since, pl.batch)
+    _i32(max_new=max_new)
     if out is None:
         out = (torch.zeros((nb, H, 2, D), dtype=K_pool.dtype, device=K_pool.device),
                torch.zeros((nb, H), dtype=torch.int32, device=K_pool.device))
@@ -673,6 +684,7 @@ def _bounds_of(bounds, mass, nb, H, D, dtype) -> None:
 
 
 def paged_select_workspace(pl: PagedLayout, max_len: int) -> int:
+    _i32(max_len=max_len)
     n = C.c_size_t(0)
     st = lib().ckv_paged_select_workspace(C.byref(pl), max_len, C.byref(n))
     if st != 0:
@@ -696,6 +708,7 @@ def paged_select(q, bounds, mass, block_table, lens, max_len: int, n_select: int
         raise ValueError("q must be a contiguous [batch, q_heads, dim] float32/bfloat16 tensor")
     _ints("block_table", block_table, q.shape[0], None)
     _ints("lens", lens, q.shape[0])
+    _i32(max_len=max_len, n_select=n_select, block_size=block_size, n_sink=n_sink, n_recent=n_recent)
     if mass.dim() != 2:
         raise ValueError("mass must be a contiguous int32 [n_blocks, heads] tensor")
     (nb, H), (B, q_heads, D) = mass.shape, q.shape
@@ -720,6 +733,7 @@ def paged_select(q, bounds, mass, block_table, lens, max_len: int, n_select: int
 
 
 def paged_sparse_decode_attn_workspace(pl: PagedLayout, q_heads: int, n_select: int) -> int:
+    _i32(q_heads=q_heads, n_select=n_select)
     n = C.c_size_t(0)
     st = lib().ckv_paged_sparse_decode_attn_workspace(C.byref(pl), q_heads, n_select, C.byref(n))
     if st != 0:
