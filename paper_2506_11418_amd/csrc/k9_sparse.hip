@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float x = (float)p.x[e];
-        qv[s][j][e] = (at < D ? x > 0.f : x < 0.f) ? 0.f : x;   // (a NaN stays one in both parts; fminf and fmaxf would drop it)
+        qv[s][j][e] = at < D ? __builtin_elementwise_minimum(x, 0.f) : __builtin_elementwise_maximum(x, 0.f);   // (a NaN stays one)
       }
     }
 
