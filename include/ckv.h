@@ -347,6 +347,10 @@ int ckv_paged_free(const int32_t* ids, int32_t n, int32_t* free_list, int32_t n_
  * layout are looked at (the others have to be positive). */
 int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int32_t n,
                     void* K_pool, void* V_pool, int32_t* deg_pool, const ckv_paged_layout* pl, void* hip_stream);
+/* The same for k and v with strides of their own (keys after their rotary embedding, values still in the projection's output). */
+int ckv_paged_write_strided(const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
+                            int64_t v_head_stride, const int32_t* slots, int32_t n, void* K_pool, void* V_pool, int32_t* deg_pool,
+                            const ckv_paged_layout* pl, void* hip_stream);
 
 /* ---- sparse decode attention over pages --------------------------------------------------------
  * A decode step that reads the n_select most promising blocks per (sequence, KV head) instead of all.

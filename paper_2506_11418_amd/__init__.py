@@ -78,7 +78,7 @@ def _binding():
         L = lib()
         m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ckv_compress, L.ckv_append, L.ckv_decode_attn, L.ckv_paged_append,
                                                        L.ckv_paged_decode_attn)))
-        m.bind_tables(*(C.cast(f, C.c_void_p).value for f in (L.ckv_paged_reserve, L.ckv_paged_trim, L.ckv_paged_write, L.ckv_paged_bounds,
+        m.bind_tables(*(C.cast(f, C.c_void_p).value for f in (L.ckv_paged_reserve, L.ckv_paged_trim, L.ckv_paged_write_strided, L.ckv_paged_bounds,
                                                               L.ckv_paged_select, L.ckv_paged_sparse_decode_attn)))
         _native = m
     return _native
@@ -128,6 +128,7 @@ def lib() -> C.CDLL:
         L.ckv_paged_trim.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp]
         L.ckv_paged_free.argtypes = [vp, i32, vp, i32, vp]
         L.ckv_paged_write.argtypes = [vp, vp, C.c_int64, C.c_int64, vp, i32, vp, vp, vp, PL, vp]
+        L.ckv_paged_write_strided.argtypes = [vp, C.c_int64, C.c_int64, vp, C.c_int64, C.c_int64, vp, i32, vp, vp, vp, PL, vp]
         L.ckv_paged_bounds.argtypes = [vp, vp, vp, vp, vp, PL, i32, vp, vp, vp]
         L.ckv_paged_select_workspace.argtypes = [PL, i32, sz]
         L.ckv_paged_select.argtypes = [vp, i32, vp, vp, vp, vp, PL, i32, i32, i32, i32, C.c_float, vp, vp, vp, C.c_size_t, vp]
@@ -612,7 +613,7 @@ def paged_free(ids, free_list) -> None:
 
 
 def paged_write(k, v, slots, K_pool, V_pool, deg_pool=None) -> None:
-    """ckv_paged_write: rows k, v [n, heads, dim] (dim contiguous, both with the same strides) into the pools at their slots, with
+    """ckv_paged_write: rows k, v [n, heads, dim] (dim contiguous, each with strides of its own) into the pools at their slots, with
     degree 1; rows of slot -1 are skipped."""
     if K_pool.is_cuda:
         st = (_native or _binding()).paged_write(k, v, slots, K_pool, V_pool, deg_pool, *_here())
@@ -626,13 +627,15 @@ def paged_write(k, v, slots, K_pool, V_pool, deg_pool=None) -> None:
     for t in (k, v):
         if tuple(t.shape) != (n, H, D) or t.dtype != K_pool.dtype or t.stride(2) != 1:
             raise ValueError("k, v must be [slots, heads, dim] tensors of the cache dtype with contiguous dim")
-    if k.stride() != v.stride():
-        raise ValueError("k and v must share strides")
     _on_this_gpu(k, v, slots, K_pool, V_pool, deg_pool)
     pl = PagedLayout(1, H, D, _DT[K_pool.dtype], bs, 1, nb)
-    row, head = (k.stride(0) if n > 1 else H * D), (k.stride(1) if H > 1 else D)
-    st = lib().ckv_paged_write(_ptr(k), _ptr(v), row, head, _ptr(slots), n, _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool), C.byref(pl),
-                               _stream())
+    # (of a single row or head, whatever stride the tensor has there)
+    ks, vs = ((t.stride(0) if n > 1 else H * D, t.stride(1) if H > 1 else D) for t in (k, v))
+    to = (_ptr(slots), n, _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool), C.byref(pl), _stream())
+    if ks == vs:
+        st = lib().ckv_paged_write(_ptr(k), _ptr(v), *ks, *to)
+    else:
+        st = lib().ckv_paged_write_strided(_ptr(k), *ks, _ptr(v), *vs, *to)
     if st != 0:
         raise CkvError(st, "ckv_paged_write")
 

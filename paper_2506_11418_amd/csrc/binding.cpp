@@ -28,7 +28,7 @@ struct Entry {
 struct Tables {
   decltype(&ckv_paged_reserve) reserve;
   decltype(&ckv_paged_trim) trim;
-  decltype(&ckv_paged_write) write;
+  decltype(&ckv_paged_write_strided) write;
   decltype(&ckv_paged_bounds) bounds;
   decltype(&ckv_paged_select) select;
   decltype(&ckv_paged_sparse_decode_attn) sparse_attn;
@@ -345,11 +345,14 @@ PyObject* paged_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
     for (const auto* t : {k, v})
       if (t->dim() != 3 || t->size(0) != rows || t->size(1) != l.heads || t->size(2) != l.dim || t->scalar_type() != type || t->stride(2) != 1)
         ok = false;
-    if (!ok || k->strides() != v->strides()) { ok = false; return 0; }
-    const int64_t row = rows > 1 ? k->stride(0) : (int64_t)l.heads * l.dim, head = l.heads > 1 ? k->stride(1) : l.dim;
+    if (!ok) return 0;
+    // (of a single row or head, whatever stride the tensor has there)
+    auto row = [&](const at::TensorBase* t) { return rows > 1 ? t->stride(0) : (int64_t)l.heads * l.dim; };
+    auto head = [&](const at::TensorBase* t) { return l.heads > 1 ? t->stride(1) : (int64_t)l.dim; };
+    const int64_t k_row = row(k), k_head = head(k), v_row = row(v), v_head = head(v);
     void *kp = ptr(k), *vp = ptr(v), *K = ptr(tensor(a[3], ok)), *V = ptr(tensor(a[4], ok)), *s = stream(a[7]);
     int32_t *sl = ptr<int32_t>(slots), *d = ptr<int32_t>(tensor(a[5], ok));
-    return unlocked([&] { return tables.write(kp, vp, row, head, sl, rows, K, V, d, &l, s); });
+    return unlocked([&] { return tables.write(kp, k_row, k_head, vp, v_row, v_head, sl, rows, K, V, d, &l, s); });
   });
 }
 
@@ -465,7 +468,7 @@ PyObject* bind_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   tables.reserve = reinterpret_cast<decltype(&ckv_paged_reserve)>(p[0]);
   tables.trim = reinterpret_cast<decltype(&ckv_paged_trim)>(p[1]);
-  tables.write = reinterpret_cast<decltype(&ckv_paged_write)>(p[2]);
+  tables.write = reinterpret_cast<decltype(&ckv_paged_write_strided)>(p[2]);
   tables.bounds = reinterpret_cast<decltype(&ckv_paged_bounds)>(p[3]);
   tables.select = reinterpret_cast<decltype(&ckv_paged_select)>(p[4]);
   tables.sparse_attn = reinterpret_cast<decltype(&ckv_paged_sparse_decode_attn)>(p[5]);

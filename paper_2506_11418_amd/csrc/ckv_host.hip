@@ -930,6 +930,12 @@ int ckv_paged_free(const int32_t* ids, int32_t n, int32_t* free_list, int32_t n_
 
 int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int32_t n,
                     void* K_pool, void* V_pool, int32_t* deg_pool, const ckv_paged_layout* pl, void* hip_stream) {
+  return ckv_paged_write_strided(k, row_stride, head_stride, v, row_stride, head_stride, slots, n, K_pool, V_pool, deg_pool, pl, hip_stream);
+}
+
+int ckv_paged_write_strided(const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v, int64_t v_row_stride,
+                            int64_t v_head_stride, const int32_t* slots, int32_t n, void* K_pool, void* V_pool, int32_t* deg_pool,
+                            const ckv_paged_layout* pl, void* hip_stream) {
   int shift;
   int st = check_paged(pl, &shift);
   if (st != CKV_OK) return st;
@@ -938,15 +944,20 @@ int ckv_paged_write(const void* k, const void* v, int64_t row_stride, int64_t he
   if ((int64_t)pl->n_blocks * pl->block_size > INT32_MAX) return CKV_EUNSUPPORTED;   // slots are 32 bits
   if (n == 0) return CKV_OK;
   if (!k || !v || !slots || !K_pool || !V_pool) return CKV_EINVAL;
-  if (head_stride < pl->dim || row_stride < pl->dim) return CKV_ESHAPE;
-  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)K_pool | (uintptr_t)V_pool) % 16 || row_stride * e % 16 || head_stride * e % 16)
-    return CKV_EALIGN;
+  for (const int64_t stride : {k_row_stride, k_head_stride, v_row_stride, v_head_stride})
+    if (stride < pl->dim) return CKV_ESHAPE;
+  if (((uintptr_t)k | (uintptr_t)v | (uintptr_t)K_pool | (uintptr_t)V_pool) % 16) return CKV_EALIGN;
+  for (const int64_t stride : {k_row_stride, k_head_stride, v_row_stride, v_head_stride})
+    if (stride * e % 16) return CKV_EALIGN;
   if (misaligned4({slots, deg_pool})) return CKV_EALIGN;
-  const size_t in = (size_t)((int64_t)(n - 1) * row_stride + (int64_t)(pl->heads - 1) * head_stride + pl->dim) * e;   // (k and v may share rows)
+  auto extent = [&](int64_t row, int64_t head) { return (size_t)((n - 1) * row + (pl->heads - 1) * head + pl->dim) * e; };
   const size_t rows = (size_t)pl->n_blocks * pl->heads * pl->block_size, pool = rows * pl->dim * e;
-  if (!writes_apart({{K_pool, pool}, {V_pool, pool}, {deg_pool, rows * 4}}, {{k, in}, {v, in}, {slots, (size_t)n * 4}})) return CKV_EINVAL;
-  return ckv::hip_status(ckv::launch_paged_write(k, v, row_stride * e, head_stride * e, slots, n, K_pool, V_pool, deg_pool, pl->heads,
-                                                 pl->dim * e, shift, pl->n_blocks, static_cast<hipStream_t>(hip_stream)));
+  if (!writes_apart({{K_pool, pool}, {V_pool, pool}, {deg_pool, rows * 4}}, 
+                    {{k, extent(k_row_stride, k_head_stride)}, {v, extent(v_row_stride, v_head_stride)}, {slots, (size_t)n * 4}}))
+    return CKV_EINVAL;                     // (k and v may share rows)
+  return ckv::hip_status(ckv::launch_paged_write(k, {k_row_stride * e, k_head_stride * e}, v, {v_row_stride * e, v_head_stride * e}, slots, n, K_pool,
+                                                 V_pool, deg_pool, pl->heads, pl->dim * e, shift, pl->n_blocks,
+                                                 static_cast<hipStream_t>(hip_stream)));
 }
 
 // ---- sparse decode attention over pages ----------------------------------------------------------

@@ -215,9 +215,9 @@ hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_
 hipError_t launch_paged_trim(int32_t* table, int32_t* lens, const int32_t* new_lens, int32_t* free_list, int n_b, int max_blocks,
                              int n_blocks, int shift, hipStream_t st);
 hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int n_blocks, hipStream_t st);
-// strides in bytes
-hipError_t launch_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int n,
-                              void* K_pool, void* V_pool, int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
+struct RowStrides { int64_t row, head; };   // in bytes
+hipError_t launch_paged_write(const void* k, RowStrides ks, const void* v, RowStrides vs, const int32_t* slots, int n, void* K_pool, void* V_pool,
+                              int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
                               hipStream_t st);
 // see k9_sparse.hip; tokens [since[b], min(lens[b], since[b] + max_new)) of every sequence, since NULL = from 0
 hipError_t launch_paged_bounds(const void* K, const int32_t* deg, int dtype, PagedView paged, const int32_t* lens, const int32_t* since,

@@ -320,9 +320,8 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
 // over and over, half of them still there, 64).
 constexpr int kWriteThreads = 256, kWritePieces = 4;
 __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
-    const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, int64_t row_stride, int64_t head_stride,
-    const int32_t* __restrict__ slots, int n, unsigned char* __restrict__ K_pool, unsigned char* __restrict__ V_pool,
-    int32_t* __restrict__ deg_pool, int heads, int pieces_per_row, int shift, int n_blocks, int rows_per_group) {
+    const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, RowStrides ks, RowStrides vs, const int32_t* __restrict__ slots, int n,
+    unsigned char* __restrict__ K_pool, unsigned char* __restrict__ V_pool, int32_t* __restrict__ deg_pool, int heads, int pieces_per_row, int shift, int n_blocks, int rows_per_group) {
   const int per_row = heads * pieces_per_row;
   const int r0 = blockIdx.x * rows_per_group, r1 = min(r0 + rows_per_group, n), total = (r1 - r0) * per_row;
   for (int e0 = threadIdx.x; e0 < total; e0 += kWriteThreads * kWritePieces) {
@@ -334,10 +333,9 @@ __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
       const int r = r0 + e / per_row, x = e % per_row;
       h[u] = x / pieces_per_row;
       piece[u] = x % pieces_per_row;
-      const int64_t from = r * row_stride + h[u] * head_stride + piece[u] * 16;
       slot[u] = slots[r];
-      a[u] = ldg16_stream(k + from);
-      c[u] = ldg16_stream(v + from);
+      a[u] = ldg16_stream(k + (r * ks.row + h[u] * ks.head + piece[u] * 16));
+      c[u] = ldg16_stream(v + (r * vs.row + h[u] * vs.head + piece[u] * 16));
     }
 #pragma unroll
     for (int u = 0; u < kWritePieces; ++u) {
@@ -390,15 +388,15 @@ hipError_t launch_paged_free(const int32_t* ids, int n, int32_t* free_list, int 
   return hipGetLastError();
 }
 
-hipError_t launch_paged_write(const void* k, const void* v, int64_t row_stride, int64_t head_stride, const int32_t* slots, int n,
-                              void* K_pool, void* V_pool, int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
+hipError_t launch_paged_write(const void* k, RowStrides ks, const void* v, RowStrides vs, const int32_t* slots, int n, void* K_pool, void* V_pool,
+                              int32_t* deg_pool, int heads, int row_bytes, int shift, int n_blocks,
                               hipStream_t st) {
   if (n == 0) return hipSuccess;
   ScopedTimer t("paged_write", st);
   const int per_row = heads * (row_bytes / 16), most = kWriteThreads * kWritePieces;
   const int rows = per_row < most ? most / per_row : 1;
   hipLaunchKernelGGL(paged_write_kernel, dim3((unsigned)div_up(n, rows)), dim3(kWriteThreads), 0, st,
-                     static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), row_stride, head_stride, slots, n,
+                     static_cast<const unsigned char*>(k), static_cast<const unsigned char*>(v), ks, vs, slots, n,
                      static_cast<unsigned char*>(K_pool), static_cast<unsigned char*>(V_pool), deg_pool, heads, row_bytes / 16, shift,
                      n_blocks, rows);
   return hipGetLastError();
