@@ -323,7 +323,7 @@ int ckv_paged_compress(void* K_pool, void* V_pool, int32_t* deg_pool, int32_t* b
  *   starts   int32 [batch + 1] or NULL: first packed token of every sequence, then their number (no entry
  *            exceeds n_slots).
  *   granted  int32 [batch] or NULL: 1 where the request was served, 0 where it was refused.
- * batch <= 4096; n_slots 0..2^30 (slots may be NULL when it is 0). */
+ * batch <= 4096, batch * max_blocks <= 2^30, max_blocks * block_size < 2^31; n_slots 0..2^30 (slots may be NULL when it is 0). */
 int ckv_paged_reserve(int32_t* block_table, int32_t* lens, const int32_t* n_new, int32_t* free_list, int32_t batch,
                       int32_t max_blocks, int32_t n_blocks, int32_t block_size, int32_t* slots, int32_t n_slots,
                       int32_t* starts, int32_t* granted, void* hip_stream);
@@ -371,9 +371,9 @@ int ckv_paged_bounds(const void* K_pool, const int32_t* deg_pool, const int32_t*
 /* The blocks to read.  Score of a block: ln(mass) + scale * max over the query heads of the KV head of
  * sum_d max(q_d lo_d, q_d hi_d), an upper bound of the logarithm of the softmax mass that Eq. 3 gives the block's
  * tokens; summed in 64 bits and rounded once to fp32, so that the selection does not hang on the order of sums.
- * The first n_sink and the last n_recent blocks of a sequence are always taken, then those whose bounds, mass or
- * query make no finite fp32 score, then the largest scores, ties to the lower block; blocks of mass <= 0 and table
- * entries outside the pool come last.
+ * The first n_sink and the last n_recent blocks of a sequence are always taken, then those without a finite score
+ * (an infinity or a NaN in their bounds or in one of the KV head's queries, or a score beyond fp32), then the largest
+ * scores, ties to the lower block; blocks of mass <= 0 and table entries outside the pool come last.
  *   lens [batch], max_len: as for ckv_paged_decode_attn.  n_sink + n_recent <= n_select.  scale <= 0 selects 1/sqrt(dim).
  *   sel int32 [batch, heads, n_select]: block * heads + head for the selected blocks in ascending order of
  *       position (-1 for one whose entry lies outside the pool), then -1.

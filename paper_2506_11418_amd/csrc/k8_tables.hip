@@ -67,7 +67,7 @@ constexpr int kReserveThreads = 256;
 //
 // What bounds it: a chain of trips to memory (lengths; entry or stack; store) and of reads of LDS, for 64 requests of one token
 // each the whole of its 4.3 us.  So a thread takes ROWS requests in a row and searches for the owners of its SLOTS slots
-// together (1000 requests, 256 at a time, slot by slot: 12.1 us, now 7.6; 33 prompts of 135000 slots 8.8, now 8.1).
+// together (1000 requests, 256 at a time, slot by slot: 12.1 us, now 7.0; 33 prompts of 135000 slots 8.8, now 7.9).
 // dynamic LDS: 12 bytes a request
 template <int ROWS, int SLOTS>   // a thread's requests and slots
 __global__ __launch_bounds__(kReserveThreads) void paged_reserve_kernel(
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(kReturnThreads) void paged_return_kernel(int32_t* _
 // Rows of k and v [n, heads, dim] into the pool by their slots (block * block_size + offset), degree 1; a slot outside the
 // pool is passed over.  A thread takes 16-byte pieces of both tensors, consecutive threads consecutive ones of a row, and asks for
 // eight before it stores one.  Bound by its bytes: 50021 rows of 8 heads of 128 bf16, 411 MB read and written, take 80 us on inputs
-// that are new each time, 5.2 TB/s, what a large copy reaches (stores that keep the pages in the caches 84; the same inputs
-// over and over, half of them still there, 64).
+// that are new each time, 5.2 TB/s, as much as torch's copy of 1 GiB (this library's row copy of 8 GiB 6.3).  Stores that keep the
+// pages in the caches 84; the same inputs over and over, half of them still there, 64.
 constexpr int kWriteThreads = 256, kWritePieces = 4;
 __global__ __launch_bounds__(kWriteThreads) void paged_write_kernel(
     const unsigned char* __restrict__ k, const unsigned char* __restrict__ v, RowStrides ks, RowStrides vs, const int32_t* __restrict__ slots, int n,
@@ -354,7 +354,10 @@ hipError_t launch_paged_reserve(int32_t* table, int32_t* lens, const int32_t* n_
                                 int n_blocks, int shift, int32_t* slots, int n_slots, int32_t* starts, int32_t* granted,
                                 hipStream_t st) {
   ScopedTimer t("paged_reserve", st);
-  const bool few = n_slots <= 32 * kReserveThreads;    // (more workgroups than that have more to do with counting themselves in)
+  // A workgroup more is one more to count itself in, a slot more of a thread lengthens its chain.  us with one / four / eight slots a
+  // thread, 33 requests: 1000 slots 4.8 / 6.2 / 8.2, 8192 5.6 / 7.1 / 9.4, 32768 6.0 / 8.0 / 10.2, 65536 7.3 / 8.0 / 10.8, 135168 10.4 /
+  // 8.2 / 10.7, 524288 28.1 / 12.5 / 12.2; 1000 requests: 4000 7.0 / 10.2 / 13.3, 65536 8.8 / 10.3 / 13.8.  (The border could be higher.)
+  const bool few = n_slots <= 32 * kReserveThreads;
   const int groups = n_slots > 0 ? div_up(n_slots, kReserveThreads * (few ? 1 : 4)) : 1;
 #define CKV_RESERVE(rows, slots_each)                                                                                      \
   hipLaunchKernelGGL((paged_reserve_kernel<rows, slots_each>), dim3((unsigned)groups), dim3(kReserveThreads), (size_t)n_b * 12, st, table, \

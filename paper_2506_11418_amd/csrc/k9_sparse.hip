@@ -133,15 +133,16 @@ __device__ __forceinline__ uint32_t rank_of(double dot, double scale, int mass) 
 // Scores, 16 blocks a wave at a time, on the 64-bit matrix instruction that takes four products of 4x4 by 4x4 (A[i][k] of product p
 // in lane i + 4p + 16k, B[k][j] in lane j + 4p + 16k, D[i][j] in lane j + 4p + 16i; checked on the GPU with whole numbers).
 // Rows i + 4p are the blocks, columns the query heads, and the contraction runs over a block's bounds as they lie in
-// memory, lo then hi: sum_d max(q_d lo_d, q_d hi_d) = sum_d min(q_d, 0) lo_d + max(q_d, 0) hi_d.  (Where that makes a NaN of zero
-// and infinity the score is not finite either way.)  A 16-byte piece of a row goes to lane block + 16 (piece % 4), and the
+// memory, lo then hi: sum_d max(q_d lo_d, q_d hi_d) = sum_d min(q_d, 0) lo_d + max(q_d, 0) hi_d for finite numbers.  An infinity or a NaN
+// in a bound or a query makes a product of the right-hand side one, and the score counts as not finite, also where the maximum
+// on the left would be (q_d above zero, lo_d = -infinity, hi_d finite).  A 16-byte piece of a row goes to lane block + 16 (piece % 4), and the
 // queries wait in fp32, as they are in 64 bits, in the order of the pieces.
 //
 // Why this instruction: the sums have to be in 64 bits (see rank_of), and it takes 16 cycles for 64 bounds and four heads where vector
 // arithmetic takes 8 for each head, and leaves four lanes to compare instead of sums over sixteen (one wave a block with vector
 // arithmetic: 100 MB 165 us, now 29).  The 16x16x4 form takes 64 cycles for sixteen columns, of which four or eight are heads.
 //
-// What bounds it: 268 MB (one sequence of 65536 blocks, 8 heads of 4) take 58 us, 4.6 TB/s.  Matrix unit busy 27 %, vector unit 38 % of the
+// What bounds it: 268 MB (one sequence of 65536 blocks, 8 heads of 4) take 58 us, 4.6 TB/s.  Matrix unit busy 26 %, vector unit 37 % of the
 // cycles (counted; they share the 64-bit arithmetic); the rest are waits for rows of 512 bytes in no order.  Neither
 // more nor fewer waves help (two workgroups a CU 63 us, four 59, six 61), nor the queries held in 64 bits (60).
 template <typename T, int D, int G>
@@ -282,8 +283,8 @@ __global__ __launch_bounds__(kScoreThreads, (score_waves<T, D, G>())) void paged
 //
 // One CU takes half a microsecond for every instruction that 65536 keys need, so that long rows are cut into segments: a
 // workgroup each finds the keys of its segment that can be among the largest, and one more takes the cut among those
-// (65536 blocks of 8 heads, 256 of them: 49 us in one step, 20 in two launches).  Short rows are bound by the chain of
-// steps between barriers: 6.4 us for 129 blocks of 8 heads, 7.0 for 2048 of 128.
+// (65536 blocks of 8 heads, 256 of them: 49 us in one step, 20 in two launches: segments 7, the cut 13).  Short rows are bound by the
+// chain of steps between barriers: 6.6 us for 129 blocks of 8 heads, 7.0 for 2048 of 128.
 enum class Step { WHOLE, SEGMENT, JOIN };
 constexpr int kBins = 2048;
 template <int THREADS>
@@ -488,8 +489,10 @@ __global__ __launch_bounds__(THREADS) void paged_select_kernel(SelectCall c) {
 
 template <typename T, int D, int G>
 hipError_t launch_scores(const SelectCall& c) {
-  // waves that run at once, three workgroups a CU, as long as each has a tile; and whole heads, so that the rows of a block that
-  // lie side by side are read together (a head a workgroup: 268 MB 67 us)
+  // Three workgroups a CU, as long as each wave has a tile; and whole heads, so that the rows of a block that lie side by side are
+  // read together (a head a workgroup: 268 MB 67 us).  Three is what runs at once of most instances; of those with fewer
+  // waves a SIMD (see score_waves) the rest is a second round (bf16, 128 channels, 61 x 8 heads of 8: 854 workgroups on 512 places).
+  // Every sequence gets the same number, whatever its length.
   const int tiles = div_up(c.key_stride, 16), fit = div_up(3 * kScoreWaves * cu_count(), c.n_b * c.heads);
   const int waves = (tiles < fit ? tiles : fit) * c.heads;
   hipLaunchKernelGGL((paged_score_kernel<T, D, G>), dim3((unsigned)div_up(waves, kScoreWaves), (unsigned)c.n_b),
@@ -553,6 +556,9 @@ hipError_t launch_paged_select(int dtype, int G, const SelectCall& c) {
   s.most = c.n_select - c.n_sink - c.n_recent;
   s.kept = c.keys + (int64_t)c.n_b * c.heads * c.key_stride;
   ScopedTimer t("paged_select", c.st);
+  // Threads and keys a thread, us on both sides of a border.  The last step of a row in segments, 512 x 8 / 1024 x 16: 2560 keys 7.5 /
+  // 10.2, 4096 8.4 / 10.8, 8192 16.7 / 12.6.  Whole rows, 256 x 8 / 1024 x 8: 1024 keys of 128 rows 6.1 / 7.7, 2048 7.0 / 7.8, 2304
+  // 10.5 / 8.0; 1024 x 8 / 1024 x 16: 4 x 8 rows of 8192 keys 8.8 / 11.0, 8 rows of 10000 14.7 / 11.5, of 16000 16.4 / 12.8.
   if (select_in_segments(c.key_stride, s.most)) {
     e = launch_select<256, kSelectSegment / 256, Step::SEGMENT>(s);
     if (e != hipSuccess) return e;

@@ -35,3 +35,12 @@ def test_numbers_of_the_calls(n):
               lambda: select(max_len=n), lambda: select(n_select=n), lambda: select(block_size=n), lambda: select(n_sink=n), lambda: select(n_recent=n)):
         with pytest.raises(ValueError, match="32 bits"):
             f()
+
+
+def test_rows_of_2_to_the_31_tokens():
+    """A row's tokens are counted in int32: wider tables are refused, so that no length and what is added to it go beyond."""
+    import ctypes as C
+    p = [C.c_void_p(i << 40) for i in range(8)]           # far apart, never followed
+    for width, block in ((1 << 21, 1024), (1 << 24, 128), (1 << 30, 2)):
+        assert ckv.lib().ckv_paged_reserve(p[1], p[2], p[3], p[4], 1, width, 50, block, p[5], 100, p[6], p[7], None) == -2
+        assert ckv.lib().ckv_paged_trim(p[1], p[2], p[3], p[4], 1, width, 50, block, None) == -2
