@@ -195,7 +195,7 @@ int ckv_decode_attn_workspace(const ckv_layout* kv, int32_t q_heads, size_t* byt
  *   o[b,h,:] = softmax( q[b,h,:] . K[b,kvh,t,:] * scale + ln deg[b,kvh,t] ) . V[b,kvh,t,:],
  *   t < lens[b], kvh = h / (q_heads / kv->heads).
  *   q [batch, q_heads, dim] contiguous, same dtype as the cache; lens [batch] int32 (each
- *   <= kv->seq; 0 gives a zero output) or NULL (= kv->seq); deg [batch, heads, kv->seq] int32
+ *   <= kv->seq; 0 gives a zero output; a NaN or +inf logit a NaN one) or NULL (= kv->seq); deg [batch, heads, kv->seq] int32
  *   (>= 1; row stride kv->deg_stride) or NULL (= 1: plain attention, Eq. 1); scale <= 0 selects 1/sqrt(dim);
  *   o [batch, q_heads, dim] contiguous in o_dtype.  Arithmetic is fp32.  One kernel launch: the
  *   sequence is split into slices, and the slice that finishes last for a (batch, KV head) merges

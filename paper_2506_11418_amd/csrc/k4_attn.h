@@ -91,9 +91,11 @@ __device__ __forceinline__ float across_lanes(float x, Op&& op) {
   return x;
 }
 
-// two neighbouring outputs: sums over the tokens divided by the sum of the weights (0 for an empty cache)
+// Sums over the tokens divided by the sum of the weights: 0 for an empty cache, NaN where a logit was no number.
+__device__ __forceinline__ float over_sum(float x, float den) { return den == 0.f ? 0.f : x / den; }
+// two neighbouring outputs
 __device__ __forceinline__ void put_out(void* __restrict__ o, int o_dtype, int64_t at, float x, float y, float den) {
-  const float rx = den > 0.f ? x / den : 0.f, ry = den > 0.f ? y / den : 0.f;
+  const float rx = over_sum(x, den), ry = over_sum(y, den);
   if (o_dtype == CKV_BF16) {
     uint16_t* op = reinterpret_cast<uint16_t*>(o) + at;
     op[0] = f32_to_bf16_rne(rx);
@@ -365,7 +367,7 @@ __device__ __forceinline__ void merge_many_slices(const float* __restrict__ o_pa
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
     const int c = tid + k * kThreads;
-    const float den = s_den[c / D], res = den > 0.f ? num[k] / den : 0.f;
+    const float res = over_sum(num[k], s_den[c / D]);
     if (o_dtype == CKV_BF16) reinterpret_cast<uint16_t*>(o)[o_base + c] = f32_to_bf16_rne(res);
     else reinterpret_cast<float*>(o)[o_base + c] = res;
   }
