@@ -394,6 +394,69 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
                                  const ckv_paged_layout* pl, int32_t n_select, float scale, void* o, int32_t o_dtype,
                                  void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- attention of several new tokens over pages ------------------------------------------------
+ * Eq. 3 for n new tokens at once: a prompt or a piece of one, a further turn on a compressed cache, drafted tokens to
+ * verify, single tokens among them.  The new tokens' keys and values are in the pages already (ckv_paged_write).
+ *   q        row i, head h at q + i * q_row_stride + h * q_head_stride (elements; dim contiguous, strides of whole 16
+ *            bytes): the new tokens of all sequences packed one behind the other, n rows; the cache's dtype.
+ *   starts   int32 [batch + 1], rising: sequence b's tokens are rows [starts[b], starts[b + 1]) (what ckv_paged_reserve
+ *            writes; entries are clamped to 0..n).  Rows of no sequence are neither read nor written.
+ *   lens     int32 [batch]: tokens of every sequence, the new ones among them, clamped to max_len and to
+ *            max_blocks * block_size.
+ *   causal   1: the new tokens are the last ones of their sequence, and each sees the tokens up to itself (one whose
+ *            place would be before the first token sees none).  0: every one sees all lens[b] tokens (cross attention to
+ *            states of another length).
+ *   scale <= 0 selects 1/sqrt(dim); CKV_EUNSUPPORTED outside 1e-30 .. 1e30.
+ *   o        [n, q_heads, dim] contiguous in o_dtype, 16-byte aligned: zero for a token that sees none; NaN where a logit
+ *            that it sees is NaN or +inf.  Tokens that it does not see (behind it, of degree 0 or below, with a table entry
+ *            outside the pool) do not reach it, whatever their keys and values hold.
+ *   workspace: scratch, whatever it holds (NULL where the size is 0); the size for an n and a max_len serves every smaller
+ *            one and every batch.  Calls that share one must not overlap in time.
+ * bf16: products on bf16 matrix instructions with fp32 sums, softmax weights rounded to bf16 (by 2^-8 at most) for the product with
+ * the values; the result does not depend on anything but the arguments (no atomics on numbers).  fp32: fp32 throughout.
+ * Supported: q_heads / heads in {1,2,4,8}; bf16 dim 64/128; fp32 dim 32/64/128; pools of fewer than 2^31 token rows;
+ * n <= 2^30. */
+int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, size_t* bytes);
+int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, const int32_t* starts, int32_t n,
+                         const void* K_pool, const void* V_pool, const int32_t* deg_pool, const int32_t* block_table, const int32_t* lens,
+                         const ckv_paged_layout* pl, int32_t max_len, float scale, int32_t causal, void* o, int32_t o_dtype, void* workspace,
+                         size_t workspace_bytes, void* hip_stream);
+
+/* ---- rows forked, pages moved -------------------------------------------------------------------
+ * Both calls settle on the table and the free list which block goes where and write the list of pairs
+ *   moves    int32 [n_moves, 2]: (from, to) block numbers, then pairs of (-1, -1),
+ * by which ckv_paged_copy then copies the pages of every pool that shares the block numbers (all layers), on the same
+ * stream and before anything else is written into them. */
+
+/* Row b continues row source[b] with blocks of its own (a block belongs to one row): it gets as many fresh blocks as that
+ * row has in the pool, in the same places, and its length.  Asked for where 0 <= source[b] < batch, source[b] != b and
+ * lens[b] == 0; rows as they were before the call are continued, any number of times.  Entries outside the pool are taken
+ * over as they are.  Requests are served in order; one is refused and left as it is where the source's length is negative
+ * or exceeds max_blocks * block_size, or where the blocks that the requests up to it need exceed those that are free, or
+ * n_moves (a refused request's blocks count; one that needs none is served).
+ *   granted  int32 [batch]: 1 where a request was served, else 0.
+ * Limits as for ckv_paged_reserve; n_moves 0..2^30 (moves may be NULL when it is 0). */
+int ckv_paged_fork(int32_t* block_table, int32_t* lens, const int32_t* source, int32_t* free_list, int32_t batch, int32_t max_blocks,
+                   int32_t n_blocks, int32_t block_size, int32_t* moves, int32_t n_moves, int32_t* granted, void* hip_stream);
+
+/* The table's blocks (entries that hold tokens, inside the pool and not free) move down: the k highest of them into the k
+ * lowest free blocks, in their order, with the largest k that leaves every one of them lower than it was, n_moves at
+ * most.  The table's entries are renamed (all that name a block, if it is named more than once), the stack of
+ * free blocks is put in order, the lowest dealt first, its rest set to -1, and word 0 to the number of blocks that are marked free.  Blocks
+ * that are in use but not in this table stay where they are.
+ *   extent   int32 [1]: one more than the highest block in use, 0 where there is none: what lies behind can be let go.
+ *   workspace: scratch, whatever it holds. */
+int ckv_paged_compact_workspace(int32_t n_blocks, size_t* bytes);
+int ckv_paged_compact(int32_t* block_table, const int32_t* lens, int32_t* free_list, int32_t batch, int32_t max_blocks, int32_t n_blocks,
+                      int32_t block_size, int32_t* moves, int32_t n_moves, int32_t* extent, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Pages moves[i][0] into pages moves[i][1]: keys, values, degrees (deg_pool may be NULL), bounds and mass (of ckv_paged_bounds;
+ * both or neither).  Pairs with a block outside the pool and pairs of equal blocks are passed over.  A block that is written
+ * must be named once; one that is written and also read by another pair leaves, piece by piece, either
+ * content there.  Of the layout batch and max_blocks are not looked at (they have to be positive).  A page's row of all heads is smaller than 2 MB. */
+int ckv_paged_copy(const int32_t* moves, int32_t n_moves, void* K_pool, void* V_pool, int32_t* deg_pool, void* bounds, int32_t* mass,
+                   const ckv_paged_layout* pl, void* hip_stream);
+
 /* Per-kernel timing for benchmarks.  When enabled, every kernel launch of the calling process
  * is bracketed by HIP events on its stream (a few microseconds per launch, on the host and on the
  * GPU: 32 attention layers lose about a quarter of their speed to it).  ckv_timing_select narrows

@@ -96,3 +96,68 @@ def select(scores, n: int, n_select: int, n_sink: int, n_recent: int):
             return (1, 0.0, i)
         return (2, -s, i)
     return sorted(sorted(range(n), key=rank)[:n_select])
+
+
+def chunk_attention(q, k, v, deg, seen, scale):
+    """Attention of new tokens over one KV head: q [n, heads, dim]; k, v [tokens, dim]; deg [tokens] (below 1: the token does not count);
+    token i sees the first seen[i] tokens.  Returns (o [n, heads, dim], a, x): a the same sums of |v|, x [n, heads] the sum
+    over channels of |q k| at its largest, for bounds of an error."""
+    n, heads, dim = q.shape
+    o, a, x = np.zeros((n, heads, dim)), np.zeros((n, heads, dim)), np.zeros((n, heads))
+    for i in range(n):
+        at = np.flatnonzero(deg[:max(int(seen[i]), 0)] > 0)
+        if not len(at):
+            continue
+        with np.errstate(all="ignore"):
+            z = q[i] @ k[at].T * scale + np.log(deg[at].astype(np.float64))
+            x[i] = (np.abs(q[i]) @ np.abs(k[at]).T).max(1)
+            for h in range(heads):
+                if np.isnan(z[h]).any() or (z[h] == np.inf).any():
+                    o[i, h] = np.nan
+                elif (z[h] > -np.inf).any():
+                    w = np.exp(z[h] - z[h].max())
+                    o[i, h], a[i, h] = w @ v[at] / w.sum(), w @ np.abs(v[at]) / w.sum()
+    return o, a, x
+
+
+def fork(table, lens, source, free: FreeList, block: int, n_moves: int):
+    """Updates table, lens and free; returns (moves, granted): pairs of block numbers, and what was served."""
+    batch, width = table.shape
+    before, old = [int(x) for x in lens], table.copy()
+    moves, granted, asked, n_free = [], [], 0, len(free.stack)
+    for b in range(batch):
+        f = int(source[b])
+        if not (0 <= f < batch and f != b and before[b] == 0 and 0 <= before[f] <= width * block):
+            granted.append(0)
+            continue
+        entries = -(-before[f] // block)
+        real = [j for j in range(entries) if 0 <= old[f, j] < free.n_blocks]
+        asked += len(real)
+        ok = not real or asked <= min(n_free, n_moves)
+        granted.append(int(ok))
+        if ok:
+            table[b, :entries] = old[f, :entries]
+            for j in real:
+                table[b, j] = free.stack.pop()
+                free.dealt.add(int(table[b, j]))
+                moves.append((int(old[f, j]), int(table[b, j])))
+            lens[b] = before[f]
+    return moves, granted
+
+
+def compact(table, lens, free: FreeList, block: int, n_moves: int):
+    """Updates table and free; returns (moves, extent)."""
+    batch, width = table.shape
+    rows = [min(max(-(-int(n) // block), 0), width) for n in lens]
+    used = sorted({int(x) for b in range(batch) for x in table[b, :rows[b]]} & free.dealt, reverse=True)
+    empty = sorted(set(range(free.n_blocks)) - free.dealt)
+    k = 0
+    while k < min(len(used), len(empty), n_moves) and used[k] > empty[k]:
+        k += 1
+    went = dict(zip(used[:k][::-1], empty[:k]))
+    for b in range(batch):
+        for j in range(rows[b]):
+            table[b, j] = went.get(int(table[b, j]), table[b, j])
+    free.dealt = (free.dealt - set(went)) | set(went.values())
+    free.stack = sorted(set(range(free.n_blocks)) - free.dealt, reverse=True)
+    return sorted(went.items()), max(free.dealt, default=-1) + 1

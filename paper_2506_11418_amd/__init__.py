@@ -80,6 +80,7 @@ def _binding():
                                                        L.ckv_paged_decode_attn)))
         m.bind_tables(*(C.cast(f, C.c_void_p).value for f in (L.ckv_paged_reserve, L.ckv_paged_trim, L.ckv_paged_write_strided, L.ckv_paged_bounds,
                                                               L.ckv_paged_select, L.ckv_paged_sparse_decode_attn)))
+        m.bind_pages(*(C.cast(f, C.c_void_p).value for f in (L.ckv_paged_chunk_attn, L.ckv_paged_fork, L.ckv_paged_compact, L.ckv_paged_copy)))
         _native = m
     return _native
 
@@ -134,6 +135,13 @@ def lib() -> C.CDLL:
         L.ckv_paged_select.argtypes = [vp, i32, vp, vp, vp, vp, PL, i32, i32, i32, i32, C.c_float, vp, vp, vp, C.c_size_t, vp]
         L.ckv_paged_sparse_decode_attn_workspace.argtypes = [PL, i32, i32, sz]
         L.ckv_paged_sparse_decode_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, PL, i32, C.c_float, vp, i32, vp, C.c_size_t, vp]
+        i64 = C.c_int64
+        L.ckv_paged_chunk_attn_workspace.argtypes = [PL, i32, i32, i32, sz]
+        L.ckv_paged_chunk_attn.argtypes = [vp, i64, i64, i32, vp, i32, vp, vp, vp, vp, vp, PL, i32, C.c_float, i32, vp, i32, vp, C.c_size_t, vp]
+        L.ckv_paged_fork.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp]
+        L.ckv_paged_compact_workspace.argtypes = [i32, sz]
+        L.ckv_paged_compact.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, i32, vp, vp, C.c_size_t, vp]
+        L.ckv_paged_copy.argtypes = [vp, i32, vp, vp, vp, vp, vp, PL, vp]
         L.ckv_bench_mfma_ceiling.argtypes = [i32, i32, i32, vp, C.c_size_t, C.POINTER(C.c_double), vp]
         L.ckv_timing_enable.argtypes = [C.c_int]
         L.ckv_timing_select.argtypes = [C.c_char_p]
@@ -775,6 +783,156 @@ def paged_sparse_decode_attn(q, K_pool, V_pool, deg_pool, sel, sel_lens, scale: 
     if st != 0:
         raise CkvError(st, "ckv_paged_sparse_decode_attn")
     return out
+
+
+# ---- attention of several new tokens over pages ------------------------------------------------
+def paged_chunk_attn_workspace(pl: PagedLayout, q_heads: int, n: int, max_len: int) -> int:
+    _i32(q_heads=q_heads, n=n, max_len=max_len)
+    b = C.c_size_t(0)
+    st = lib().ckv_paged_chunk_attn_workspace(C.byref(pl), q_heads, n, max_len, C.byref(b))
+    if st != 0:
+        raise CkvError(st, "ckv_paged_chunk_attn_workspace")
+    return b.value
+
+
+def paged_chunk_attn(q, K_pool, V_pool, deg_pool, block_table, lens, starts, max_len: int, scale: float = 0.0, causal: bool = True,
+                     out_dtype=None, out=None, workspace=None):
+    """ckv_paged_chunk_attn: Eq. 3 for the new tokens q [n, q_heads, dim] (dim contiguous, rows and heads with strides of their own) of
+    all sequences, sequence b's at rows [starts[b], starts[b + 1]) (as paged_reserve returns them), whose keys and values
+    paged_write has put into the pages; lens counts them.  Each sees its sequence up to itself, without `causal` all of it.
+    Returns o [n, q_heads, dim]; rows of no sequence are not written (zero where `out` is not passed)."""
+    if out is not None and workspace is not None and q.is_cuda:
+        st = (_native or _binding()).paged_chunk_attn(q, K_pool, V_pool, deg_pool, block_table, lens, starts, max_len, scale, causal, out,
+                                                      workspace, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_chunk_attn")
+    nb, H, bs, D = _pools(K_pool, V_pool, deg_pool)
+    if q.dim() != 3 or q.dtype != K_pool.dtype or q.shape[2] != D or q.stride(2) != 1:
+        raise ValueError("q must be a [tokens, q_heads, dim] tensor of the cache dtype with contiguous dim")
+    n, q_heads = q.shape[:2]
+    pl = paged_layout_of(K_pool, block_table)
+    _ints("lens", lens, pl.batch)
+    _ints("starts", starts, pl.batch + 1)
+    _i32(n=n, q_heads=q_heads, max_len=max_len)
+    if out is None:
+        out = torch.zeros(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    if out.shape != q.shape or not out.is_contiguous() or out.dtype not in _DT:
+        raise ValueError("out must be a contiguous float32/bfloat16 tensor of the query's shape")
+    if workspace is None:
+        workspace = torch.empty(paged_chunk_attn_workspace(pl, q_heads, n, max_len), dtype=torch.uint8, device=q.device)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _on_this_gpu(q, K_pool, V_pool, deg_pool, block_table, lens, starts, out, workspace)
+    # (of a single row or head, whatever stride the tensor has there)
+    row, head = q.stride(0) if n > 1 else q_heads * D, q.stride(1) if q_heads > 1 else D
+    st = lib().ckv_paged_chunk_attn(_ptr(q), row, head, q_heads, _ptr(starts), n, _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool),
+                                    _ptr(block_table), _ptr(lens), C.byref(pl), max_len, scale, 1 if causal else 0, _ptr(out),
+                                    _DT[out.dtype], _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_chunk_attn")
+    return out
+
+
+# ---- rows forked, pages moved ------------------------------------------------------------------
+def paged_fork(block_table, lens, source, free_list, block_size: int, n_moves: int, out: Optional[tuple] = None):
+    """ckv_paged_fork: every empty row b with source[b] >= 0 continues that row with blocks of its own.  Updates block_table, lens and
+    free_list and returns (moves [n_moves, 2], granted [batch]); the pages follow by paged_copy(moves, ...) of every pool.
+    n_moves: the blocks of all rows asked for, or more.  `out` may pass preallocated (moves, granted)."""
+    if out is not None and block_table.is_cuda:
+        st = (_native or _binding()).paged_fork(block_table, lens, source, free_list, block_size, n_moves, *out, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_fork")
+    _ints("block_table", block_table, None, None)
+    B, width = block_table.shape
+    n_blocks = _pool_blocks(free_list)
+    _ints("lens", lens, B)
+    _ints("source", source, B)
+    _i32(block_size=block_size, n_moves=n_moves)
+    if n_moves < 0:
+        raise ValueError("n_moves must not be negative")
+    if out is None:
+        out = (torch.empty((n_moves, 2), dtype=torch.int32, device=block_table.device), torch.empty(B, dtype=torch.int32, device=block_table.device))
+    moves, granted = out
+    _ints("moves", moves, n_moves, 2)
+    _ints("granted", granted, B)
+    _on_this_gpu(block_table, lens, source, free_list, moves, granted)
+    st = lib().ckv_paged_fork(_ptr(block_table), _ptr(lens), _ptr(source), _ptr(free_list), B, width, n_blocks, block_size, _ptr(moves),
+                              n_moves, _ptr(granted), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_fork")
+    return moves, granted
+
+
+def paged_compact_workspace(n_blocks: int) -> int:
+    _i32(n_blocks=n_blocks)
+    b = C.c_size_t(0)
+    st = lib().ckv_paged_compact_workspace(n_blocks, C.byref(b))
+    if st != 0:
+        raise CkvError(st, "ckv_paged_compact_workspace")
+    return b.value
+
+
+def paged_compact(block_table, lens, free_list, block_size: int, n_moves: int, out: Optional[tuple] = None,
+                  workspace: Optional[torch.Tensor] = None):
+    """ckv_paged_compact: the table's highest blocks move into the lowest free ones, n_moves at most.  Updates block_table and free_list
+    and returns (moves [n_moves, 2], extent [1]: one more than the highest block in use); the pages follow by paged_copy(moves,
+    ...) of every pool.  `out` may pass both, `workspace` scratch of paged_compact_workspace() bytes."""
+    if out is not None and workspace is not None and block_table.is_cuda:
+        st = (_native or _binding()).paged_compact(block_table, lens, free_list, block_size, n_moves, *out, workspace, *_here())
+        if st == 0:
+            return out
+        if st is not None:
+            raise CkvError(st, "ckv_paged_compact")
+    _ints("block_table", block_table, None, None)
+    B, width = block_table.shape
+    n_blocks = _pool_blocks(free_list)
+    _ints("lens", lens, B)
+    _i32(block_size=block_size, n_moves=n_moves)
+    if n_moves < 0:
+        raise ValueError("n_moves must not be negative")
+    if out is None:
+        out = (torch.empty((n_moves, 2), dtype=torch.int32, device=block_table.device), torch.empty(1, dtype=torch.int32, device=block_table.device))
+    moves, extent = out
+    _ints("moves", moves, n_moves, 2)
+    _ints("extent", extent, 1)
+    if workspace is None:
+        workspace = torch.empty(paged_compact_workspace(n_blocks), dtype=torch.uint8, device=block_table.device)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _on_this_gpu(block_table, lens, free_list, moves, extent, workspace)
+    st = lib().ckv_paged_compact(_ptr(block_table), _ptr(lens), _ptr(free_list), B, width, n_blocks, block_size, _ptr(moves), n_moves,
+                                 _ptr(extent), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_compact")
+    return moves, extent
+
+
+def paged_copy(moves, K_pool, V_pool, deg_pool=None, bounds=None, mass=None) -> None:
+    """ckv_paged_copy: pages moves[i, 0] into pages moves[i, 1] of the pools (and of bounds and mass, both or neither); pairs of -1 are
+    passed over.  Call it for every pool that shares the block numbers, before anything else is written into them."""
+    if K_pool.is_cuda:
+        st = (_native or _binding()).paged_copy(moves, K_pool, V_pool, deg_pool, bounds, mass, *_here())
+        if st == 0:
+            return
+        if st is not None:
+            raise CkvError(st, "ckv_paged_copy")
+    nb, H, bs, D = _pools(K_pool, V_pool, deg_pool)
+    _ints("moves", moves, None, 2)
+    if (bounds is None) != (mass is None):
+        raise ValueError("bounds and mass go together")
+    if bounds is not None:
+        _bounds_of(bounds, mass, nb, H, D, K_pool.dtype)
+    _i32(moves=moves.shape[0])
+    _on_this_gpu(moves, K_pool, V_pool, deg_pool, bounds, mass)
+    pl = PagedLayout(1, H, D, _DT[K_pool.dtype], bs, 1, nb)
+    st = lib().ckv_paged_copy(_ptr(moves), moves.shape[0], _ptr(K_pool), _ptr(V_pool), _ptr(deg_pool), _ptr(bounds), _ptr(mass), C.byref(pl),
+                              _stream())
+    if st != 0:
+        raise CkvError(st, "ckv_paged_copy")
 
 
 def mfma_ceiling(mode: int, waves_per_cu: int, iters: int = 20000) -> float:

@@ -34,6 +34,13 @@ struct Tables {
   decltype(&ckv_paged_sparse_decode_attn) sparse_attn;
 } tables;
 
+struct Pages {
+  decltype(&ckv_paged_chunk_attn) chunk_attn;
+  decltype(&ckv_paged_fork) fork;
+  decltype(&ckv_paged_compact) compact;
+  decltype(&ckv_paged_copy) copy;
+} pages;
+
 // a tensor argument: NULL for None; `ok` turns false for what this file does not take
 const at::TensorBase* tensor(PyObject* x, bool& ok) {
   if (x == Py_None) return nullptr;
@@ -430,6 +437,94 @@ PyObject* paged_sparse_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n) 
   });
 }
 
+// q, K_pool, V_pool, deg_pool, block_table, lens, starts, max_len, scale, causal, out, workspace, device, stream
+PyObject* paged_chunk_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 14, [&](bool& ok) -> int {
+    const Here at{small_int(a[12], ok), ok};
+    const auto *q = at.need(a[0]), *out = at.need(a[10]), *ws = at.need(a[11]);
+    ckv_paged_layout l = pools(at, a[1], a[2], a[3]);
+    const auto* table = at.ints(a[4], {-1, -1});
+    const int32_t max_len = small_int(a[7], ok);
+    const float scale = number(a[8], ok);
+    if (!PyBool_Check(a[9])) ok = false;
+    if (!ok || q->dim() != 3 || q->stride(2) != 1 || q->size(2) != l.dim || q->scalar_type() != (l.dtype == CKV_BF16 ? at::kBFloat16 : at::kFloat) ||
+        !out->is_contiguous() || out->sizes() != q->sizes() || !ws->is_contiguous()) {
+      ok = false;
+      return 0;
+    }
+    l.batch = fits(table->size(0), ok);
+    l.max_blocks = fits(table->size(1), ok);
+    const auto *lens = at.ints(a[5], {l.batch}), *starts = at.ints(a[6], {(int64_t)l.batch + 1});
+    const int32_t rows = fits(q->size(0), ok), heads = fits(q->size(1), ok);
+    const int o_type = dtype_of(*out, ok);
+    if (!ok) return 0;
+    // (of a single row or head, whatever stride the tensor has there)
+    const int64_t q_row = rows > 1 ? q->stride(0) : (int64_t)heads * l.dim, q_head = heads > 1 ? q->stride(1) : (int64_t)l.dim;
+    const int32_t causal = a[9] == Py_True;
+    void *qp = ptr(q), *K = ptr(tensor(a[1], ok)), *V = ptr(tensor(a[2], ok)), *o = ptr(out), *w = ptr(ws), *s = stream(a[13]);
+    int32_t *d = ptr<int32_t>(tensor(a[3], ok)), *t = ptr<int32_t>(table), *ls = ptr<int32_t>(lens), *s0 = ptr<int32_t>(starts);
+    const size_t nw = bytes_of(ws);
+    return unlocked([&] {
+      return pages.chunk_attn(qp, q_row, q_head, heads, s0, rows, K, V, d, t, ls, &l, max_len, scale, causal, o, o_type, w, nw, s);
+    });
+  });
+}
+
+// block_table, lens, source, free_list, block_size, n_moves, moves, granted, device, stream
+PyObject* paged_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&](bool& ok) -> int {
+    const Here at{small_int(a[8], ok), ok};
+    const auto *table = at.ints(a[0], {-1, -1}), *list = at.ints(a[3], {-1});
+    if (!ok) return 0;
+    const int32_t bs = small_int(a[4], ok), n_moves = small_int(a[5], ok), blocks = listed_blocks(list, ok);
+    const int32_t batch = fits(table->size(0), ok), width = fits(table->size(1), ok);
+    if (n_moves < 0) ok = false;
+    const auto *lens = at.ints(a[1], {batch}), *source = at.ints(a[2], {batch}), *moves = at.ints(a[6], {n_moves, 2}), *granted = at.ints(a[7], {batch});
+    if (!ok) return 0;
+    int32_t *t = ptr<int32_t>(table), *l = ptr<int32_t>(lens), *f = ptr<int32_t>(list), *sr = ptr<int32_t>(source), *m = ptr<int32_t>(moves);
+    int32_t* g = ptr<int32_t>(granted);
+    void* s = stream(a[9]);
+    return unlocked([&] { return pages.fork(t, l, sr, f, batch, width, blocks, bs, m, n_moves, g, s); });
+  });
+}
+
+// block_table, lens, free_list, block_size, n_moves, moves, extent, workspace, device, stream
+PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&](bool& ok) -> int {
+    const Here at{small_int(a[8], ok), ok};
+    const auto *table = at.ints(a[0], {-1, -1}), *list = at.ints(a[2], {-1}), *ws = at.need(a[7]);
+    if (!ok || !ws->is_contiguous()) { ok = false; return 0; }
+    const int32_t bs = small_int(a[3], ok), n_moves = small_int(a[4], ok), blocks = listed_blocks(list, ok);
+    const int32_t batch = fits(table->size(0), ok), width = fits(table->size(1), ok);
+    if (n_moves < 0) ok = false;
+    const auto *lens = at.ints(a[1], {batch}), *moves = at.ints(a[5], {n_moves, 2}), *extent = at.ints(a[6], {1});
+    if (!ok) return 0;
+    int32_t *t = ptr<int32_t>(table), *l = ptr<int32_t>(lens), *f = ptr<int32_t>(list), *m = ptr<int32_t>(moves), *e = ptr<int32_t>(extent);
+    void *w = ptr(ws), *s = stream(a[9]);
+    const size_t nw = bytes_of(ws);
+    return unlocked([&] { return pages.compact(t, l, f, batch, width, blocks, bs, m, n_moves, e, w, nw, s); });
+  });
+}
+
+// moves, K_pool, V_pool, deg_pool, bounds, mass, device, stream
+PyObject* paged_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&](bool& ok) -> int {
+    const Here at{small_int(a[6], ok), ok};
+    const auto *moves = at.ints(a[0], {-1, 2}), *bounds = at.take(a[4]), *mass = at.ints(a[5], {-1, -1}, true);
+    const ckv_paged_layout l = pools(at, a[1], a[2], a[3]);
+    if (!ok || !bounds != !mass || (bounds && (mass->size(0) != l.n_blocks || mass->size(1) != l.heads ||
+                                               !bounds_fit(bounds, mass, l.dtype == CKV_BF16 ? at::kBFloat16 : at::kFloat, l.dim)))) {
+      ok = false;
+      return 0;
+    }
+    const int32_t n_moves = fits(moves->size(0), ok);
+    if (!ok) return 0;
+    void *K = ptr(tensor(a[1], ok)), *V = ptr(tensor(a[2], ok)), *b = ptr(bounds), *s = stream(a[7]);
+    int32_t *mv = ptr<int32_t>(moves), *d = ptr<int32_t>(tensor(a[3], ok)), *ms = ptr<int32_t>(mass);
+    return unlocked([&] { return pages.copy(mv, n_moves, K, V, d, b, ms, &l, s); });
+  });
+}
+
 // the addresses of the library's entry points, in Entry's order
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 5) {
@@ -475,11 +570,33 @@ PyObject* bind_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// the same for Pages
+PyObject* bind_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "four addresses");
+    return nullptr;
+  }
+  void* p[4];
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
+      return nullptr;
+    }
+  }
+  pages.chunk_attn = reinterpret_cast<decltype(&ckv_paged_chunk_attn)>(p[0]);
+  pages.fork = reinterpret_cast<decltype(&ckv_paged_fork)>(p[1]);
+  pages.compact = reinterpret_cast<decltype(&ckv_paged_compact)>(p[2]);
+  pages.copy = reinterpret_cast<decltype(&ckv_paged_copy)>(p[3]);
+  Py_RETURN_NONE;
+}
+
 #define CKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CKV_METHOD(bind), CKV_METHOD(compress), CKV_METHOD(append), CKV_METHOD(decode_attn),
                          CKV_METHOD(paged_append), CKV_METHOD(paged_decode_attn), CKV_METHOD(bind_tables),
                          CKV_METHOD(paged_reserve), CKV_METHOD(paged_trim), CKV_METHOD(paged_write), CKV_METHOD(paged_bounds),
-                         CKV_METHOD(paged_select), CKV_METHOD(paged_sparse_decode_attn), {nullptr, nullptr, 0, nullptr}};
+                         CKV_METHOD(paged_select), CKV_METHOD(paged_sparse_decode_attn), CKV_METHOD(bind_pages),
+                         CKV_METHOD(paged_chunk_attn), CKV_METHOD(paged_fork), CKV_METHOD(paged_compact), CKV_METHOD(paged_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ckv_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

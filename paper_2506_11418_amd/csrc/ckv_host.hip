@@ -1086,6 +1086,130 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
                                o, o_dtype, workspace, workspace_bytes, hip_stream);
 }
 
+// ---- attention of several new tokens over pages --------------------------------------------------
+namespace {
+int check_chunk(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, int* shift) {
+  const int st = check_sparse(pl, shift);    // (dims, pool rows and launch dimensions as there)
+  if (st != CKV_OK) return st;
+  if (q_heads <= 0 || q_heads % pl->heads || n < 0 || max_len <= 0) return CKV_ESHAPE;
+  const int G = q_heads / pl->heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return CKV_EUNSUPPORTED;
+  if (n > kMostEntries) return CKV_EUNSUPPORTED;
+  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, max_len);
+  if ((int64_t)cut.slots * pl->heads * cut.splits > INT32_MAX || (int64_t)n * q_heads / 4 >= INT32_MAX) return CKV_EUNSUPPORTED;   // workgroups of a launch
+  return CKV_OK;
+}
+}  // namespace
+
+int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, size_t* bytes) {
+  int shift;
+  const int st = check_chunk(pl, q_heads, n, max_len, &shift);
+  if (st != CKV_OK) return st;
+  if (!bytes) return CKV_EINVAL;
+  *bytes = ckv::align_up(ckv::chunk_reserve_bytes(pl->heads, q_heads, n, max_len, pl->dim), 256);
+  return CKV_OK;
+}
+
+int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, const int32_t* starts, int32_t n,
+                         const void* K_pool, const void* V_pool, const int32_t* deg_pool, const int32_t* block_table, const int32_t* lens,
+                         const ckv_paged_layout* pl, int32_t max_len, float scale, int32_t causal, void* o, int32_t o_dtype, void* workspace,
+                         size_t workspace_bytes, void* hip_stream) {
+  int shift;
+  const int st = check_chunk(pl, q_heads, n, max_len, &shift);
+  if (st != CKV_OK) return st;
+  if (o_dtype != CKV_F32 && o_dtype != CKV_BF16) return CKV_EINVAL;
+  if (n == 0) return CKV_OK;
+  if (!q || !starts || !K_pool || !V_pool || !block_table || !lens || !o) return CKV_EINVAL;
+  const int e = ckv::elem_bytes(pl->dtype);
+  if (q_row_stride < pl->dim || q_head_stride < pl->dim) return CKV_ESHAPE;
+  if (((uintptr_t)q | (uintptr_t)K_pool | (uintptr_t)V_pool | (uintptr_t)o | (uintptr_t)workspace) % 16 || q_row_stride * e % 16 ||
+      q_head_stride * e % 16 || misaligned4({starts, deg_pool, block_table, lens}))
+    return CKV_EALIGN;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)pl->dim);
+  if (!(scale >= 1e-30f && scale <= 1e30f)) return CKV_EUNSUPPORTED;         // (ln N / scale is a number)
+  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, max_len);
+  const int64_t heads = (int64_t)n * q_heads;
+  const size_t need = ckv::chunk_workspace_bytes(heads, cut.splits, pl->dim);
+  if (need && !workspace) return CKV_EINVAL;
+  if (workspace_bytes < need) return CKV_EWORKSPACE;
+  const size_t row = (size_t)pl->dim * e, rows = (size_t)pl->n_blocks * pl->heads * pl->block_size, b4 = (size_t)pl->batch * 4;
+  if (!writes_apart({{o, (size_t)heads * pl->dim * ckv::elem_bytes(o_dtype)}, {workspace, need}},
+                    {{q, (size_t)((n - 1) * q_row_stride + (q_heads - 1) * q_head_stride + pl->dim) * e}, {K_pool, rows * row}, {V_pool, rows * row},
+                     {deg_pool, rows * 4}, {block_table, b4 * pl->max_blocks}, {lens, b4}, {starts, b4 + 4}}))
+    return CKV_EINVAL;
+  ckv::ChunkCall c{};
+  c.q = q; c.q_row = q_row_stride * e; c.q_head = q_head_stride * e;
+  c.q_heads = q_heads; c.n = n; c.n_b = pl->batch; c.heads = pl->heads;
+  c.starts = starts;
+  c.K = K_pool; c.V = V_pool; c.deg = deg_pool;
+  c.paged = ckv::PagedView{block_table, pl->max_blocks, shift, pl->n_blocks};
+  c.lens = lens; c.max_len = max_len; c.causal = causal != 0;
+  c.scale = scale;
+  c.o = o; c.o_dtype = o_dtype;
+  c.workspace = workspace;
+  return ckv::hip_status(ckv::launch_chunk_attn(c, pl->dtype, pl->dim, static_cast<hipStream_t>(hip_stream)));
+}
+
+// ---- rows forked, pages moved --------------------------------------------------------------------
+int ckv_paged_fork(int32_t* block_table, int32_t* lens, const int32_t* source, int32_t* free_list, int32_t batch, int32_t max_blocks,
+                   int32_t n_blocks, int32_t block_size, int32_t* moves, int32_t n_moves, int32_t* granted, void* hip_stream) {
+  int shift;
+  const int st = check_tables(batch, max_blocks, n_blocks, block_size, &shift);
+  if (st != CKV_OK) return st;
+  if (n_moves < 0 || n_moves > kMostEntries) return CKV_ESHAPE;
+  if (!block_table || !lens || !source || !free_list || (!moves && n_moves > 0) || !granted) return CKV_EINVAL;
+  if (misaligned4({block_table, lens, source, free_list, moves, granted})) return CKV_EALIGN;
+  const size_t n = (size_t)batch * 4;
+  if (!apart({{block_table, n * max_blocks}, {lens, n}, {source, n}, {free_list, 16 + (size_t)n_blocks * 8}, {moves, (size_t)n_moves * 8}, {granted, n}}))
+    return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_fork(block_table, lens, source, free_list, batch, max_blocks, n_blocks, shift, moves, n_moves, granted,
+                                                static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_compact_workspace(int32_t n_blocks, size_t* bytes) {
+  if (n_blocks <= 0) return CKV_ESHAPE;
+  if (n_blocks > kMostEntries) return CKV_EUNSUPPORTED;
+  if (!bytes) return CKV_EINVAL;
+  *bytes = ckv::align_up(ckv::compact_scratch_bytes(n_blocks), 256);
+  return CKV_OK;
+}
+
+int ckv_paged_compact(int32_t* block_table, const int32_t* lens, int32_t* free_list, int32_t batch, int32_t max_blocks, int32_t n_blocks,
+                      int32_t block_size, int32_t* moves, int32_t n_moves, int32_t* extent, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int shift;
+  const int st = check_tables(batch, max_blocks, n_blocks, block_size, &shift);
+  if (st != CKV_OK) return st;
+  if (n_moves < 0 || n_moves > kMostEntries) return CKV_ESHAPE;
+  if (!block_table || !lens || !free_list || (!moves && n_moves > 0) || !extent || !workspace) return CKV_EINVAL;
+  if ((uintptr_t)workspace % 16 || misaligned4({block_table, lens, free_list, moves, extent})) return CKV_EALIGN;
+  const size_t need = ckv::compact_scratch_bytes(n_blocks), n = (size_t)batch * 4;
+  if (workspace_bytes < need) return CKV_EWORKSPACE;
+  if (!apart({{block_table, n * max_blocks}, {lens, n}, {free_list, 16 + (size_t)n_blocks * 8}, {moves, (size_t)n_moves * 8}, {extent, 4}, {workspace, need}}))
+    return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_compact(block_table, lens, free_list, batch, max_blocks, n_blocks, shift, moves, n_moves, extent, workspace,
+                                                   static_cast<hipStream_t>(hip_stream)));
+}
+
+int ckv_paged_copy(const int32_t* moves, int32_t n_moves, void* K_pool, void* V_pool, int32_t* deg_pool, void* bounds, int32_t* mass,
+                   const ckv_paged_layout* pl, void* hip_stream) {
+  int shift;
+  const int st = check_paged(pl, &shift);
+  if (st != CKV_OK) return st;
+  const int e = ckv::elem_bytes(pl->dtype);
+  const int64_t page = (int64_t)pl->heads * pl->block_size * pl->dim * e;
+  if (n_moves < 0 || n_moves > kMostEntries || (int64_t)pl->heads * pl->dim * e > INT32_MAX / 1024) return CKV_ESHAPE;
+  if ((page / 16384 + 1) * n_moves > INT32_MAX) return CKV_EUNSUPPORTED;     // workgroups of a launch
+  if (n_moves == 0) return CKV_OK;
+  if (!moves || !K_pool || !V_pool || !bounds != !mass) return CKV_EINVAL;
+  if (((uintptr_t)K_pool | (uintptr_t)V_pool | (uintptr_t)bounds) % 16 || misaligned4({moves, deg_pool, mass})) return CKV_EALIGN;
+  const size_t n = (size_t)pl->n_blocks, pairs = n * pl->heads;
+  if (!apart({{moves, (size_t)n_moves * 8}, {K_pool, n * page}, {V_pool, n * page}, {deg_pool, pairs * pl->block_size * 4},
+              {bounds, pairs * 2 * pl->dim * e}, {mass, pairs * 4}}))
+    return CKV_EINVAL;
+  return ckv::hip_status(ckv::launch_paged_copy(moves, n_moves, K_pool, V_pool, deg_pool, bounds, mass, pl->n_blocks, pl->heads, pl->block_size,
+                                                pl->dim * e, static_cast<hipStream_t>(hip_stream)));
+}
+
 int ckv_timing_enable(int on) {
   if (!on) fold_launches();
   g_timing = on != 0;

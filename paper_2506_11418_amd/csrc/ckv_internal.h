@@ -246,6 +246,37 @@ inline size_t select_words(int key_stride) {
 }
 hipError_t launch_paged_select(int dtype, int G, const SelectCall& c);
 
+// see k10_chunk.hip: attention of the new tokens [starts[b], starts[b + 1]) of every sequence over its pages
+struct ChunkCall {
+  const void* q;
+  int64_t q_row, q_head;       // in bytes
+  int q_heads, n, n_b, heads;
+  const int32_t* starts;
+  const void *K, *V;
+  const int32_t* deg;
+  PagedView paged;
+  const int32_t* lens;
+  int max_len, causal;
+  float scale;
+  void* o;
+  int o_dtype;
+  void* workspace;
+};
+struct ChunkCut { int slots, splits; };   // places for workgroups' rows, parts that the tokens are cut into
+ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len);
+size_t chunk_workspace_bytes(int64_t rows, int splits, int dim);                                     // of this very call
+size_t chunk_reserve_bytes(int heads, int q_heads, int n, int max_len, int dim);   // enough for every call of up to that many tokens, any batch
+hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t st);
+
+// see k11_pages.hip
+hipError_t launch_paged_fork(int32_t* table, int32_t* lens, const int32_t* source, int32_t* free_list, int n_b, int max_blocks, int n_blocks,
+                             int shift, int32_t* moves, int n_moves, int32_t* granted, hipStream_t st);
+size_t compact_scratch_bytes(int n_blocks);
+hipError_t launch_paged_compact(int32_t* table, const int32_t* lens, int32_t* free_list, int n_b, int max_blocks, int n_blocks, int shift,
+                                int32_t* moves, int n_moves, int32_t* extent, void* workspace, hipStream_t st);
+hipError_t launch_paged_copy(const int32_t* moves, int n_moves, void* K, void* V, int32_t* deg, void* bounds, int32_t* mass, int n_blocks, int heads,
+                             int block_size, int row_bytes, hipStream_t st);
+
 // ---- timing hooks ----------------------------------------------------------------------------
 // One-time set-up of a kernel that needs more than the default dynamic LDS, per device (each device
 // holds its own copy of the code object, so the limit is raised on each one that launches it).

@@ -1,0 +1,510 @@
+// Attention of several new tokens of every sequence over a block-paged cache (Eq. 3 for each of them):
+//   o_i = softmax_t(q_i . k_t * scale + ln N_t) V,   t up to the token's own position (or over the whole cache).
+// The rows of one KV head's product are (new token, query head of the group) pairs, so that keys and values are read once for the
+// group.  A workgroup takes 128 rows of one sequence and walks over its tokens in tiles that go from memory to LDS without
+// passing registers; a wave holds 32 rows: their queries, their running maximum and sum, and their sums of values.
+//
+// The product is turned: S^T = K Q^T has a query row in each lane, so that the softmax of a row is a matter of one lane and its
+// partner 32 lanes away, and what comes out of it is, without any exchange, the right operand of O^T += V^T P^T: the order in which
+// the tokens of a matrix instruction are summed is free, and V is read from LDS in the order P has.
+#include <type_traits>
+
+#include "ckv_internal.h"
+#include "ckv_device.h"
+#include "k4_attn.h"
+
+namespace ckv {
+namespace {
+
+constexpr int kRows = 128;               // query rows of a workgroup
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr float kSlack = 8.f;            // how far (log2) a logit may exceed the reference before the sums are rescaled
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+struct ChunkArgs {
+  const unsigned char* q;
+  int64_t q_row, q_head;                 // in bytes
+  int n, n_b;
+  const int32_t* starts;
+  const unsigned char *K, *V;
+  const int32_t* deg;
+  PagedView paged;
+  const int32_t* lens;
+  int max_len, heads, g_shift;           // query heads per KV head = 1 << g_shift
+  float c;                               // scale * log2 e
+  int causal, splits, slots;
+  void* o;
+  int o_dtype;
+  float *o_part, *ml_part;               // [split][token][query head][dim] and [..][2], with more than one split
+};
+
+// What a tile of the cache looks like for each type.  PIECES: 16-byte pieces of a row; TILE: tokens.
+template <typename T, int D>
+struct Tile {
+  static constexpr bool BF16 = std::is_same<T, __bf16>::value;
+  static constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16;
+  static constexpr int SUB = BF16 ? 2 : 1;               // 32-token products of a tile
+  static constexpr int TILE = 32 * SUB;
+  static constexpr int BYTES = TILE * RB;
+  static constexpr int ROWS_PER_LOAD = 64 / PIECES;      // of a wave
+  static constexpr int LOADS = TILE / ROWS_PER_LOAD / kWaves;
+  static_assert(LOADS * ROWS_PER_LOAD * kWaves == TILE, "whole loads per wave");
+  // Which 16-byte slot of its row piece p sits in (an involution).  Keys: 16 rows, one piece of each, in different banks.  Values:
+  // bf16, four rows of 64 bytes (a transposed read of half a wave); fp32, rows four apart, 128 bytes of each.
+  __device__ static __forceinline__ int k_slot(int row, int p) { return p ^ (PIECES >= 16 ? row & 15 : (row >> 1) & 7); }
+  __device__ static __forceinline__ int v_slot(int row, int p) {
+    if constexpr (BF16) return p ^ ((PIECES == 16 ? row & 3 : (row >> 1) & 1) << 2);
+    else return PIECES >= 16 ? p ^ (((row >> 2) & 1) << 3) : p;
+  }
+};
+
+// 16 bytes a lane from memory into LDS, lane l's at lds + 16 l (lds: the same in all lanes).  As a builtin every later read of LDS
+// would wait for it; here the wait is the one before the tile's barrier.
+__device__ __forceinline__ void to_lds16(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// op over a lane and its partner 32 away
+template <class Op>
+__device__ __forceinline__ float with_partner(float x, Op&& op) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
+  using L = Tile<T, D>;
+  constexpr int SUB = L::SUB, DT = D / 32;
+  extern __shared__ __attribute__((aligned(16))) unsigned char s_tiles[];     // two tiles of keys and values
+  __shared__ __attribute__((aligned(16))) float s_bias[2][L::TILE];
+  __shared__ uint64_t s_valid[2], s_odd;                 // a tile's tokens that count; those with a value that is no finite number
+  __shared__ int s_seq;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+
+  // ---- which rows, which tokens
+  const int id = blockIdx.x;
+  const int kvh = id % a.heads, split = (id / a.heads) % a.splits, slot = a.slots - 1 - id / a.heads / a.splits;
+  const int t_shift = __builtin_ctz(kRows) - a.g_shift;  // tokens of a workgroup
+  // Sequence b has the slots from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
+  if (tid == 0) s_seq = 0;
+  __syncthreads();
+  int before = 0;
+  for (int b = tid; b < a.n_b; b += kThreads) before += (min(max(a.starts[b], 0), a.n) >> t_shift) + b <= slot;
+  if (before) atomicAdd(&s_seq, before);
+  __syncthreads();
+  const int b = s_seq - 1;
+  if (b < 0) return;
+  const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
+  const int tok0 = first + ((slot - (first >> t_shift) - b) << t_shift);
+  const int tokens = min(last - tok0, 1 << t_shift);
+  if (tokens <= 0) return;
+  const int64_t cap = (int64_t)a.paged.max_blocks << a.paged.shift;
+  const int len = (int)min((int64_t)min(max(a.lens[b], 0), a.max_len), cap);
+  const int pos0 = len - (last - tok0);                  // position of the first of these tokens
+  const int rows = tokens << a.g_shift;
+  const int row = wave * 32 + col;
+  const bool live = row < rows;
+  const int my_tok = min(row >> a.g_shift, tokens - 1), my_head = (kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1));
+  const int limit = a.causal ? pos0 + my_tok : len - 1;  // the last token that this row sees
+  const int seen = a.causal ? max(min(pos0 + tokens, len), 0) : len;          // tokens that any row sees
+  const int all_see = a.causal ? pos0 : len - 1;         // the last one that every row sees
+  const int wave_last = a.causal ? pos0 + min((wave * 32 + 31) >> a.g_shift, tokens - 1) : len - 1;
+  const bool idle = wave * 32 >= rows;
+
+  const int n_tiles = (seen + L::TILE - 1) / L::TILE;
+  const int tile0 = (int)((int64_t)n_tiles * split / a.splits), tile1 = (int)((int64_t)n_tiles * (split + 1) / a.splits);
+  const int32_t* table = a.paged.table + (int64_t)b * a.paged.max_blocks;
+  const int shift = a.paged.shift, mask = (1 << shift) - 1;
+
+  // ---- queries: lane (col, half) holds pieces 2 s + half of its row
+  constexpr int QP = L::PIECES / 2;
+  uint4 qf[QP];
+  {
+    const unsigned char* qr = a.q + (int64_t)(tok0 + my_tok) * a.q_row + (int64_t)my_head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < QP; ++s) qf[s] = *reinterpret_cast<const uint4*>(qr + (2 * s + half) * 16);
+  }
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  float ref = -INFINITY, sum = 0.f;
+
+  // ---- staging.  A lane's rows of a tile: ROWS_PER_LOAD rows a load, wave w's loads one behind the other.
+  const int r0 = wave * L::LOADS * L::ROWS_PER_LOAD + lane / L::PIECES, slot_in_row = lane % L::PIECES;
+  auto entry = [&](int t) { return table[min(t, seen - 1) >> shift]; };
+  auto pool_row = [&](int e, int t) -> int64_t {        // (an entry outside the pool: row 0, masked)
+    return (unsigned)e < (unsigned)a.paged.n_blocks ? (((int64_t)e * a.heads + kvh) << shift) + (min(t, seen - 1) & mask) : 0;
+  };
+  int ent[L::LOADS], ent_d = 0;
+  auto ask_entries = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) ent[i] = entry(tile * L::TILE + r0 + i * L::ROWS_PER_LOAD);
+    if (wave == kWaves - 1) ent_d = entry(tile * L::TILE + (lane & (L::TILE - 1)));
+  };
+  const uint32_t lds0 = lds_address(s_tiles);
+  int dg = 1;
+  auto request = [&](int tile, int buf) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)buf * 2 * L::BYTES + (uint32_t)wave * L::LOADS * 1024);
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const int r = r0 + i * L::ROWS_PER_LOAD;
+      const int64_t at = pool_row(ent[i], tile * L::TILE + r) * L::RB;
+      to_lds16(a.K + at + L::k_slot(r, slot_in_row) * 16, to + i * 1024);
+      to_lds16(a.V + at + L::v_slot(r, slot_in_row) * 16, to + L::BYTES + i * 1024);
+    }
+    if (wave == kWaves - 1 && a.deg) dg = a.deg[pool_row(ent_d, tile * L::TILE + (lane & (L::TILE - 1)))];
+  };
+  // what the last wave says of a tile's tokens: ln N / scale of each (the product's first addend), and which count
+  auto describe = [&](int tile, int buf, int e) {
+    if (wave == kWaves - 1) {
+      const int i = lane & (L::TILE - 1);
+      const bool ok = tile * L::TILE + i < seen && (unsigned)e < (unsigned)a.paged.n_blocks && dg > 0;
+      if (a.deg && lane < L::TILE) s_bias[buf][i] = ok ? __log2f((float)dg) / a.c : 0.f;
+      const uint64_t valid = __ballot(ok);
+      if (lane == 0) s_valid[buf] = valid;
+    }
+  };
+
+  if (tile0 < tile1) {
+    ask_entries(tile0);
+    request(tile0, 0);
+    const int e0 = ent_d;
+    ask_entries(tile0 + 1);
+    describe(tile0, 0, e0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  for (int tile = tile0; tile < tile1; ++tile) {
+    const int buf = (tile - tile0) & 1, t0 = tile * L::TILE;
+    const bool more = tile + 1 < tile1;
+    const int e_next = ent_d;
+    if (more) {
+      request(tile + 1, buf ^ 1);
+      ask_entries(tile + 2);
+    }
+    unsigned char* sk = s_tiles + buf * 2 * L::BYTES;
+    unsigned char* sv = sk + L::BYTES;
+    const uint64_t valid = ((uint64_t)__builtin_amdgcn_readfirstlane((int)(s_valid[buf] >> 32)) << 32) |
+                           (uint32_t)__builtin_amdgcn_readfirstlane((int)s_valid[buf]);
+    const bool edge = t0 + L::TILE - 1 > all_see || valid != ~0ull;
+    uint64_t odd = 0;
+    if (edge) {
+      // Some row must not see some token: a weight of zero is no mask where the value is no finite number.  Values of tokens
+      // that do not count become zero; so do infinities and NaN, which are added to the rows that see them afterwards.
+      if (tid == 0) s_odd = 0;
+      __syncthreads();
+      for (int p = tid; p < L::TILE * L::PIECES; p += kThreads) {
+        const int r = p / L::PIECES;
+        uint4* at = reinterpret_cast<uint4*>(sv) + p;
+        uint4 u = *at;
+        uint32_t* w = reinterpret_cast<uint32_t*>(&u);
+        bool changed = false, strange = false;
+        if (!((valid >> r) & 1)) {
+          u = make_uint4(0, 0, 0, 0);
+          changed = true;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t keep = ~0u;
+            if constexpr (L::BF16) {
+              if ((w[i] & 0x7f80u) == 0x7f80u) keep &= 0xffff0000u;
+              if ((w[i] & 0x7f800000u) == 0x7f800000u) keep &= 0x0000ffffu;
+            } else {
+              if ((w[i] & 0x7f800000u) == 0x7f800000u) keep = 0;
+            }
+            if (keep != ~0u) { w[i] &= keep; strange = true; }
+          }
+        }
+        if (changed || strange) *at = u;
+        if (strange) atomicOr(reinterpret_cast<unsigned long long*>(&s_odd), 1ull << r);
+      }
+      __syncthreads();
+      odd = ((uint64_t)__builtin_amdgcn_readfirstlane((int)(s_odd >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)s_odd);
+    }
+    if (!idle && t0 <= wave_last) {
+      // ---- S^T: lane (col, half), register i: token 8 (i / 4) + 4 half + i % 4 of its 32
+      f32x16 s[SUB];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        if (a.deg) {
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(&s_bias[buf][u * 32 + 8 * i4 + 4 * half]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[u][4 * i4 + i] = v[i];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+        }
+        const int r = u * 32 + col;
+#pragma unroll
+        for (int st = 0; st < QP; ++st) {
+          const uint4 kf = *reinterpret_cast<const uint4*>(sk + r * L::RB + L::k_slot(r, 2 * st + half) * 16);
+          if constexpr (L::BF16) {
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[st]), s[u], 0, 0, 0);
+          } else {
+            const f32x4 kk = __builtin_bit_cast(f32x4, kf), qq = __builtin_bit_cast(f32x4, qf[st]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[j], qq[j], s[u], 0, 0, 0);
+          }
+        }
+      }
+      if (edge) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = u * 32 + 8 * (i >> 2) + (i & 3) + 4 * half;
+            if (t0 + j > limit || !((valid >> j) & 1)) s[u][i] = -INFINITY;
+          }
+      }
+      // ---- softmax against a reference that follows the maximum once it is 2^8 below it
+      float top = s[0][0];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+      top = with_partner(top, [](float x, float y) { return fmaxf(x, y); }) * a.c;
+      if (__any(top > ref + kSlack)) {
+        const float now = fmaxf(ref, top);
+        const float f = now == -INFINITY ? 1.f : exp2_raw(ref - now);
+        ref = now;
+        sum *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+      }
+      const float base = ref == -INFINITY ? 0.f : ref;   // (a row that has seen nothing yet: all weights zero)
+      if constexpr (L::BF16) {
+        // Weights are rounded to bf16 for the product: 2^-8 of each at most, and their sum is taken of the rounded ones, so that they
+        // still add up to one.
+        const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            Piece p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f32x2 w = {exp2_raw(fmaf(s[u][8 * k + 2 * i], a.c, -base)), exp2_raw(fmaf(s[u][8 * k + 2 * i + 1], a.c, -base))};
+              p.p[i] = __builtin_convertvector(w, bf16x2);
+              sum = __builtin_amdgcn_fdot2_f32_bf16(p.p[i], ones, sum, false);
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+              // lanes 16 g .. 16 g + 15 read a 4 x 16 block: tokens 4 half + .., channels 16 (g & 1) + ..
+              union { s16x4 h[2]; bf16x8 v; } vt;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int r = u * 32 + 16 * k + 8 * e + 4 * half + ((lane & 15) >> 2);
+                const int at = 64 * d + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+                vt.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(sv + r * L::RB + L::v_slot(r, at >> 4) * 16 + (at & 8)));
+              }
+              acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt.v, p.v, acc[d], 0, 0, 0);
+            }
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float w = exp2_raw(fmaf(s[0][i], a.c, -base));
+          sum += w;
+          const int r = 8 * (i >> 2) + 4 * half + (i & 3);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const int at = 128 * d + 4 * col;
+            const float v = *reinterpret_cast<const float*>(sv + r * L::RB + L::v_slot(r, at >> 4) * 16 + (at & 15));
+            acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w, acc[d], 0, 0, 0);
+          }
+        }
+      }
+      // ---- values that are no finite numbers, as they are in the cache
+      while (odd) {
+        const int j = __builtin_ctzll(odd);
+        odd &= odd - 1;
+        const int t = t0 + j;
+        const unsigned char* vr = a.V + pool_row(entry(t), t) * L::RB;
+        if (t <= limit) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int ch = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
+              float v;
+              if constexpr (L::BF16) v = __uint_as_float((uint32_t) reinterpret_cast<const uint16_t*>(vr)[ch] << 16);
+              else v = reinterpret_cast<const float*>(vr)[ch];
+              if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) acc[d][i] += v;
+            }
+        }
+      }
+    }
+    if (more) describe(tile + 1, buf ^ 1, e_next);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  if (idle) return;
+  sum = with_partner(sum, [](float x, float y) { return x + y; });
+  if (!live) return;
+  const int64_t out_row = (int64_t)(tok0 + my_tok) * (a.heads << a.g_shift) + my_head;
+  if (a.splits == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const int64_t at = out_row * D + 32 * d + 8 * i4 + 4 * half;
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = sum == 0.f ? 0.f : acc[d][4 * i4 + i] * inv;
+        if (a.o_dtype == CKV_BF16) {
+          const f32x2 lo = {v[0], v[1]}, hi = {v[2], v[3]};
+          const uint2 w = make_uint2(__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+                                     __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2)));
+          *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.o) + at) = w;
+        } else {
+          *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.o) + at) = v;
+        }
+      }
+    return;
+  }
+  const int64_t part = (int64_t)split * a.n * (a.heads << a.g_shift) + out_row;
+  if (half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part]) = make_float2(ref, sum);
+  if (tile0 >= tile1) return;            // (nothing is read there: its weight is zero)
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = acc[d][4 * i4 + i];
+      *reinterpret_cast<f32x4*>(&a.o_part[part * D + 32 * d + 8 * i4 + 4 * half]) = v;
+    }
+}
+
+// The splits of a row put together, in the order of their numbers: a wave takes a row, a lane D / 64 channels (D = 32: half of the
+// lanes one each).
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ ml_part, int splits, int64_t n_rows, int q_heads,
+                                                          const int32_t* __restrict__ starts, int n_b, int n, void* __restrict__ o, int o_dtype) {
+  constexpr int E = D == 128 ? 2 : 1;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= n_rows) return;
+  const int tok = (int)(row / q_heads);
+  if (tok < starts[0] || tok >= min(starts[n_b], n)) return;
+  float m = -INFINITY, l = 0.f;
+  if (lane < splits) {
+    const float2 v = *reinterpret_cast<const float2*>(&ml_part[2 * (lane * n_rows + row)]);
+    m = v.x;
+    l = v.y;
+  }
+  const float top = across_lanes<0x3f>(m, [](float x, float y) { return fmaxf(x, y); });
+  const float w = m == -INFINITY ? 0.f : exp2f(m - top);
+  const float den = across_lanes<0x3f>(w * l, [](float x, float y) { return x + y; });
+  float x[E] = {};
+  for (int s = 0; s < splits; ++s) {
+    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+    if (f == 0.f) continue;
+    const float* p = &o_part[(s * n_rows + row) * D + E * (lane & (D / E - 1))];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = fmaf(p[e], f, x[e]);
+  }
+  if (E * lane >= D) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float r = over_sum(x[e], den);
+    if (o_dtype == CKV_BF16) reinterpret_cast<uint16_t*>(o)[row * D + E * lane + e] = f32_to_bf16_rne(r);
+    else reinterpret_cast<float*>(o)[row * D + E * lane + e] = r;
+  }
+}
+
+}  // namespace
+
+namespace {
+constexpr int kMostSplits = 64, kLeastSpan = 256;
+int most_splits(int max_len) { return max_len >= kMostSplits * kLeastSpan ? kMostSplits : div_up(max_len, kLeastSpan); }
+int wanted_groups() { return 2 * cu_count(); }
+}  // namespace
+
+ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
+  ChunkCut cut;
+  cut.slots = n / (kRows / (q_heads / heads)) + n_b;
+  const int64_t groups = (int64_t)cut.slots * heads, s = (wanted_groups() + groups - 1) / groups;
+  cut.splits = (int)(s < most_splits(max_len) ? s : most_splits(max_len));
+  return cut;
+}
+
+// (max, sum) pairs, up to the next 16 bytes, then the sums of values
+size_t chunk_workspace_bytes(int64_t rows, int splits, int dim) {
+  if (splits <= 1) return 0;
+  const size_t parts = (size_t)rows * splits;
+  return (parts * 8 + 15) / 16 * 16 + parts * dim * 4;
+}
+
+// Where a call is split, its places are fewer than wanted_groups() / heads: it has fewer than kRows * wanted_groups() rows, and as
+// many parts of rows again as make up the difference.
+size_t chunk_reserve_bytes(int heads, int q_heads, int n, int max_len, int dim) {
+  const int most = most_splits(max_len);
+  const int64_t full = (int64_t)kRows * wanted_groups(), rows = (int64_t)n * q_heads, cut = rows < full ? rows : full;
+  const int64_t parts = cut * most < full + cut ? cut * most : full + cut;
+  return most <= 1 ? 0 : chunk_workspace_bytes(parts, 2, dim) / 2 + 16;
+}
+
+hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t st) {
+  const ChunkCut cut = chunk_cut(c.n_b, c.heads, c.q_heads, c.n, c.max_len);
+  ChunkArgs a{};
+  a.q = static_cast<const unsigned char*>(c.q);
+  a.q_row = c.q_row; a.q_head = c.q_head;
+  a.n = c.n; a.n_b = c.n_b; a.starts = c.starts;
+  a.K = static_cast<const unsigned char*>(c.K); a.V = static_cast<const unsigned char*>(c.V); a.deg = c.deg;
+  a.paged = c.paged; a.lens = c.lens; a.max_len = c.max_len; a.heads = c.heads;
+  a.g_shift = __builtin_ctz(c.q_heads / c.heads);
+  a.c = c.scale * kLog2e;
+  a.causal = c.causal; a.splits = cut.splits; a.slots = cut.slots;
+  a.o = c.o; a.o_dtype = c.o_dtype;
+  const int64_t rows = (int64_t)c.n * c.q_heads;
+  a.ml_part = static_cast<float*>(c.workspace);
+  a.o_part = a.ml_part + (rows * cut.splits * 2 + 3) / 4 * 4;
+  const dim3 grid((unsigned)((int64_t)cut.slots * c.heads * cut.splits));
+  hipError_t e = hipErrorInvalidValue;
+#define CKV_CHUNK(T, D)                                                                                               \
+  do {                                                                                                                \
+    static KernelSetup setup;                                                                                         \
+    constexpr size_t lds = 4 * Tile<T, D>::BYTES;                                                                     \
+    e = kernel_setup(reinterpret_cast<const void*>(&chunk_attn_kernel<T, D>), lds, setup);                            \
+    if (e != hipSuccess) return e;                                                                                    \
+    {                                                                                                                 \
+      ScopedTimer t("chunk_attn", st);                                                                                \
+      hipLaunchKernelGGL((chunk_attn_kernel<T, D>), grid, dim3(kThreads), lds, st, a);                                \
+    }                                                                                                                 \
+    e = hipGetLastError();                                                                                            \
+    if (e == hipSuccess && cut.splits > 1) {                                                                          \
+      ScopedTimer t("chunk_merge", st);                                                                               \
+      hipLaunchKernelGGL((chunk_merge_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a.o_part, a.ml_part, \
+                         cut.splits, rows, c.q_heads, c.starts, c.n_b, c.n, c.o, c.o_dtype);                          \
+      e = hipGetLastError();                                                                                          \
+    }                                                                                                                 \
+  } while (0)
+  if (dtype == CKV_BF16) {
+    if (dim == 64) CKV_CHUNK(__bf16, 64);
+    else if (dim == 128) CKV_CHUNK(__bf16, 128);
+  } else {
+    if (dim == 32) CKV_CHUNK(float, 32);
+    else if (dim == 64) CKV_CHUNK(float, 64);
+    else if (dim == 128) CKV_CHUNK(float, 128);
+  }
+#undef CKV_CHUNK
+  return e;
+}
+
+}  // namespace ckv

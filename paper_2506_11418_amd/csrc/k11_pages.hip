@@ -1,0 +1,379 @@
+// Rows of a block table forked and blocks moved: which block a page goes to is settled on the table and the free list (see
+// k8_tables.hip for its layout), and the pages of every pool that shares them are then copied by the list of pairs.
+#include "ckv_internal.h"
+#include "ckv_device.h"
+
+namespace ckv {
+namespace {
+
+constexpr int kListHead = 4;
+constexpr int kInUse = INT32_MAX;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+
+__device__ __forceinline__ int blocks_of(int tokens, int shift) { return (tokens >> shift) + ((tokens & ((1 << shift) - 1)) != 0); }
+// entries of a row that hold tokens
+__device__ __forceinline__ int entries_of(int len, int max_blocks, int shift) { return min(blocks_of(max(len, 0), shift), max_blocks); }
+
+// Sum of x over the threads before this one; `all` receives that over the whole workgroup.  s_wave: one word a wave.
+template <int THREADS>
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* s_wave, uint32_t& all) {
+  const uint32_t upto = wave_inclusive_scan(x);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 63) s_wave[wave] = upto;
+  __syncthreads();
+  uint32_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w == wave) before = all;
+    all += s_wave[w];
+  }
+  __syncthreads();
+  return before + upto - x;
+}
+
+// ---- fork ----------------------------------------------------------------------------------------
+// need[b] := blocks of the row that row b continues, -1 where none is asked for or it cannot be.
+__global__ __launch_bounds__(64) void fork_count_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
+                                                        const int32_t* __restrict__ source, int n_b, int max_blocks, int n_blocks, int shift,
+                                                        int32_t* __restrict__ need) {
+  const int b = blockIdx.x, lane = threadIdx.x, f = source[b];
+  int count = -1;
+  if ((unsigned)f < (unsigned)n_b && f != b && lens[b] == 0) {
+    const int len = lens[f];
+    if (len >= 0 && len <= (int64_t)max_blocks << shift) {
+      count = 0;
+      const int32_t* row = table + (int64_t)f * max_blocks;
+      for (int j = lane; j < blocks_of(len, shift); j += 64) count += (unsigned)row[j] < (unsigned)n_blocks;
+      for (int w = 1; w < 64; w *= 2) count += __shfl_xor(count, w);
+    }
+  }
+  if (lane == 0) need[b] = count;
+}
+
+// Every workgroup sums the rows' needs for itself and deals to its share of the rows; the last one to arrive writes what the others
+// have read: lengths, grants (which held the needs) and the number of free blocks.
+// dynamic LDS: 4 bytes a row
+template <int ROWS>   // rows of a thread's sums
+__global__ __launch_bounds__(kThreads) void fork_deal_kernel(int32_t* __restrict__ table, int32_t* __restrict__ lens,
+                                                             const int32_t* __restrict__ source, int32_t* __restrict__ free_list, int n_b,
+                                                             int max_blocks, int n_blocks, int shift, int32_t* __restrict__ moves, int n_moves,
+                                                             int32_t* __restrict__ granted) {
+  extern __shared__ int32_t s_end[];
+  __shared__ uint32_t s_wave[kWaves];
+  __shared__ int s_last, s_take;
+  const int tid = threadIdx.x;
+  const int n_free = min(max(free_list[0], 0), n_blocks), most = min(n_free, n_moves);
+  const int32_t* stack = free_list + kListHead;
+  int32_t* marks = free_list + kListHead + n_blocks;
+  int need[ROWS];
+  uint32_t mine = 0, all;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    need[r] = tid * ROWS + r < n_b ? max(granted[tid * ROWS + r], 0) : 0;
+    mine += need[r];
+  }
+  if (tid == 0) s_take = 0;
+  uint32_t end = sum_before<kThreads>(mine, s_wave, all);
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    end += need[r];
+    if (tid * ROWS + r < n_b) s_end[tid * ROWS + r] = (int)end;
+    if (need[r] > 0 && end <= (uint32_t)most) atomicMax(&s_take, (int)end);
+  }
+  __syncthreads();
+  const int take = s_take;
+  for (int b = blockIdx.x; b < n_b; b += gridDim.x) {
+    const int base = b ? s_end[b - 1] : 0;
+    if (granted[b] < 0 || (s_end[b] > base && s_end[b] > most)) continue;   // not asked for, or refused
+    const int f = source[b], entries = blocks_of(lens[f], shift);
+    const int32_t* from = table + (int64_t)f * max_blocks;
+    int32_t* to = table + (int64_t)b * max_blocks;
+    int dealt = base;
+    for (int j0 = 0; j0 < entries; j0 += kThreads) {
+      const int j = j0 + tid, id = j < entries ? from[j] : -1;
+      const bool real = (unsigned)id < (unsigned)n_blocks;
+      uint32_t here;
+      const int at = dealt + (int)sum_before<kThreads>(real, s_wave, here);
+      int fresh = id;
+      if (real && at < s_end[b]) {
+        fresh = stack[n_free - 1 - at];
+        moves[2 * at] = id;
+        moves[2 * at + 1] = fresh;
+        if ((unsigned)fresh < (unsigned)n_blocks) marks[fresh] = kInUse;
+      }
+      if (j < entries) to[j] = fresh;
+      dealt += (int)here;
+    }
+  }
+  for (int64_t i = 2 * (int64_t)take + blockIdx.x * kThreads + tid; i < 2 * (int64_t)n_moves; i += (int64_t)gridDim.x * kThreads) moves[i] = -1;
+  __syncthreads();                         // (what this workgroup read has arrived: it has been stored or compared)
+  if (tid == 0) s_last = gridDim.x == 1 || atomicAdd(&free_list[1], 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!s_last) return;
+  // A row that is itself asked for was empty: what continues it is so too, whatever it becomes in this call.
+  int len[ROWS], ok[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int b = tid + r * kThreads;
+    len[r] = ok[r] = 0;
+    if (b < n_b) {
+      const int asked = granted[b];
+      ok[r] = asked == 0 || (asked > 0 && s_end[b] <= most);
+      if (ok[r] && granted[source[b]] < 0) len[r] = lens[source[b]];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int b = tid + r * kThreads;
+    if (b < n_b) {
+      if (len[r] > 0) lens[b] = len[r];
+      granted[b] = ok[r];
+    }
+  }
+  if (tid == 0) {
+    free_list[0] = n_free - take;
+    if (gridDim.x > 1) atomicExch(&free_list[1], 0);
+  }
+}
+
+// ---- compact -------------------------------------------------------------------------------------
+// Two bits a block, in words of 32: free, and named by the table (and not free); before each word, how many of either.  With them
+// everything is a matter of counting: the k highest of the table's blocks move into the k lowest free ones, k as large as leaves every
+// one lower than it was.
+struct CompactScratch {
+  uint32_t *free, *used, *free_before, *used_before;
+  int32_t* head;                           // k, free blocks, the table's blocks
+};
+
+__global__ __launch_bounds__(kThreads) void compact_free_kernel(const int32_t* __restrict__ free_list, int n_blocks, CompactScratch w,
+                                                                int32_t* __restrict__ extent) {
+  const int x = blockIdx.x * kThreads + threadIdx.x;
+  const int32_t* marks = free_list + kListHead + n_blocks;
+  const uint64_t bits = __ballot(x < n_blocks && marks[min(x, n_blocks - 1)] == -1);
+  if ((threadIdx.x & 31) == 0 && x < n_blocks) {
+    w.free[x >> 5] = (threadIdx.x & 32) ? (uint32_t)(bits >> 32) : (uint32_t)bits;
+    w.used[x >> 5] = 0;
+  }
+  if (x == 0) *extent = 0;
+}
+
+__global__ __launch_bounds__(kThreads) void compact_used_kernel(const int32_t* __restrict__ table, const int32_t* __restrict__ lens, int max_blocks,
+                                                                int n_blocks, int shift, CompactScratch w) {
+  const int b = blockIdx.x, entries = entries_of(lens[b], max_blocks, shift);
+  const int32_t* row = table + (int64_t)b * max_blocks;
+  for (int j = blockIdx.y * kThreads + threadIdx.x; j < entries; j += gridDim.y * kThreads) {
+    const int id = row[j];
+    if ((unsigned)id < (unsigned)n_blocks && !((w.free[id >> 5] >> (id & 31)) & 1)) atomicOr(&w.used[id >> 5], 1u << (id & 31));
+  }
+}
+
+constexpr int kScanThreads = 1024;
+__global__ __launch_bounds__(kScanThreads) void compact_scan_kernel(int words, int n_moves, CompactScratch w) {
+  __shared__ uint32_t s_wave[kScanThreads / 64];
+  __shared__ int s_k;
+  const int tid = threadIdx.x;
+  uint32_t n_free = 0, n_used = 0;
+  for (int w0 = 0; w0 < words; w0 += kScanThreads) {
+    const int i = w0 + tid;
+    uint32_t all;
+    const uint32_t f = sum_before<kScanThreads>(i < words ? __popc(w.free[i]) : 0, s_wave, all) + n_free;
+    n_free += all;
+    const uint32_t u = sum_before<kScanThreads>(i < words ? __popc(w.used[i]) : 0, s_wave, all) + n_used;
+    n_used += all;
+    if (i < words) {
+      w.free_before[i] = f;
+      w.used_before[i] = u;
+    }
+  }
+  if (tid == 0) s_k = 0;
+  __syncthreads();                         // (a thread reads the words that it has written)
+  // free ones below a block rise, the table's from there on fall: the largest minimum of the two lies where they cross
+  int k = 0;
+  for (int i = tid; i < words; i += kScanThreads) {
+    uint32_t below = w.free_before[i], above = n_used - w.used_before[i];
+    const uint32_t f = w.free[i], u = w.used[i];
+    k = max(k, (int)min(below, above));
+    if (below < above && below + __popc(f) >= above - __popc(u))
+      for (int bit = 0; bit < 32; ++bit) {
+        below += (f >> bit) & 1;
+        above -= (u >> bit) & 1;
+        k = max(k, (int)min(below, above));
+      }
+  }
+  if (k) atomicMax(&s_k, k);
+  __syncthreads();
+  if (tid == 0) {
+    w.head[0] = min(s_k, n_moves);
+    w.head[1] = (int)n_free;
+    w.head[2] = (int)n_used;
+  }
+}
+
+__device__ __forceinline__ uint32_t upto_bit(uint32_t word, int bit) { return word & ((1u << bit) - 1); }
+
+// moves, marks and the stack of free blocks, the lowest of them dealt first
+__global__ __launch_bounds__(kThreads) void compact_blocks_kernel(int32_t* __restrict__ free_list, int n_blocks, CompactScratch w,
+                                                                  int32_t* __restrict__ moves, int n_moves, int32_t* __restrict__ extent) {
+  const int x = blockIdx.x * kThreads + threadIdx.x;
+  const int k = w.head[0], n_free = w.head[1], n_used = w.head[2];
+  int32_t* stack = free_list + kListHead;
+  int32_t* marks = stack + n_blocks;
+  bool taken = false;
+  if (x < n_blocks) {
+    const int i = x >> 5, bit = x & 31;
+    const uint32_t f = w.free[i], u = w.used[i];
+    const int free_below = (int)(w.free_before[i] + __popc(upto_bit(f, bit))), used_below = (int)(w.used_before[i] + __popc(upto_bit(u, bit)));
+    const int moved_below = max(used_below - (n_used - k), 0);            // the k highest move
+    const bool home = ((f >> bit) & 1) && free_below < k, mover = ((u >> bit) & 1) && used_below >= n_used - k;
+    if (home) {
+      moves[2 * free_below + 1] = x;
+      marks[x] = kInUse;
+    }
+    if (mover) {
+      moves[2 * moved_below] = x;
+      marks[x] = -1;
+    }
+    const bool free_now = mover || (((f >> bit) & 1) && !home);
+    if (free_now) stack[n_free - 1 - (free_below - min(free_below, k) + moved_below)] = x;
+    if (x >= n_free) stack[x] = -1;
+    taken = !free_now;
+  }
+  const uint64_t some = __ballot(taken);
+  if (some && (threadIdx.x & 63) == 0) atomicMax(extent, x + 64 - (int)__builtin_clzll(some));
+  for (int64_t i = 2 * (int64_t)k + x; i < 2 * (int64_t)n_moves; i += (int64_t)gridDim.x * kThreads) moves[i] = -1;
+  if (x == 0) free_list[0] = n_free;
+}
+
+__global__ __launch_bounds__(kThreads) void compact_rename_kernel(int32_t* __restrict__ table, const int32_t* __restrict__ lens, int max_blocks,
+                                                                  int n_blocks, int shift, CompactScratch w, const int32_t* __restrict__ moves) {
+  const int b = blockIdx.x, entries = entries_of(lens[b], max_blocks, shift), k = w.head[0], n_used = w.head[2];
+  int32_t* row = table + (int64_t)b * max_blocks;
+  for (int j = blockIdx.y * kThreads + threadIdx.x; j < entries; j += gridDim.y * kThreads) {
+    const int id = row[j];
+    if ((unsigned)id >= (unsigned)n_blocks) continue;
+    const uint32_t u = w.used[id >> 5];
+    const int above = n_used - (int)(w.used_before[id >> 5] + __popc(upto_bit(u, id & 31)));
+    if (((u >> (id & 31)) & 1) && above <= k) row[j] = moves[2 * (k - above) + 1];
+  }
+}
+
+// ---- copy ----------------------------------------------------------------------------------------
+// Pages by pairs (from, to).  A workgroup takes kPieces 16-byte pieces of the keys and of the values: of several pages where they are
+// small (`group` of them), else part of one.
+constexpr int kPerThread = 4, kPieces = kThreads * kPerThread;
+__global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __restrict__ moves, int n_moves, unsigned char* __restrict__ K,
+                                                              unsigned char* __restrict__ V, int32_t* __restrict__ deg, unsigned char* __restrict__ bounds,
+                                                              int32_t* __restrict__ mass, int n_blocks, int page_pieces, int rows, int heads,
+                                                              int bound_pieces, int group, int parts) {
+  const int m0 = blockIdx.x / parts * group, part = blockIdx.x % parts, tid = threadIdx.x;
+  const int n = min(group, n_moves - m0);
+  auto pair = [&](int m, int& from, int& to) {
+    from = moves[2 * m];
+    to = moves[2 * m + 1];
+    return (unsigned)from < (unsigned)n_blocks && (unsigned)to < (unsigned)n_blocks && from != to;
+  };
+  const int p0 = part * kPieces, total = parts > 1 ? min(kPieces, page_pieces - p0) : n * page_pieces;
+  uint4 k[kPerThread], v[kPerThread];
+  int64_t at[kPerThread];
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    const int e = tid + i * kThreads;
+    at[i] = -1;
+    if (e < total) {
+      const int m = parts > 1 ? 0 : e / page_pieces, p = parts > 1 ? p0 + e : e % page_pieces;
+      int from, to;
+      if (pair(m0 + m, from, to)) {
+        at[i] = ((int64_t)to * page_pieces + p) * 16;
+        const int64_t src = ((int64_t)from * page_pieces + p) * 16;
+        k[i] = ldg16_stream(K + src);
+        v[i] = ldg16_stream(V + src);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i)
+    if (at[i] >= 0) {
+      stg16_stream(K + at[i], k[i]);
+      stg16_stream(V + at[i], v[i]);
+    }
+  if (part) return;
+  for (int m = 0; m < n; ++m) {
+    int from, to;
+    if (!pair(m0 + m, from, to)) continue;
+    if (deg)
+      for (int i = tid; i < rows; i += kThreads) deg[(int64_t)to * rows + i] = deg[(int64_t)from * rows + i];
+    if (bounds) {
+      for (int i = tid; i < bound_pieces; i += kThreads)
+        *reinterpret_cast<uint4*>(bounds + ((int64_t)to * bound_pieces + i) * 16) = *reinterpret_cast<const uint4*>(bounds + ((int64_t)from * bound_pieces + i) * 16);
+      for (int i = tid; i < heads; i += kThreads) mass[(int64_t)to * heads + i] = mass[(int64_t)from * heads + i];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_fork(int32_t* table, int32_t* lens, const int32_t* source, int32_t* free_list, int n_b, int max_blocks, int n_blocks,
+                             int shift, int32_t* moves, int n_moves, int32_t* granted, hipStream_t st) {
+  {
+    ScopedTimer t("fork_count", st);
+    hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)n_b), dim3(64), 0, st, table, lens, source, n_b, max_blocks, n_blocks, shift, granted);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  ScopedTimer t("fork_deal", st);
+  const dim3 grid((unsigned)(n_b < 256 ? n_b : 256));
+  if (n_b <= kThreads)
+    hipLaunchKernelGGL(fork_deal_kernel<1>, grid, dim3(kThreads), (size_t)n_b * 4, st, table, lens, source, free_list, n_b, max_blocks, n_blocks, shift,
+                       moves, n_moves, granted);
+  else
+    hipLaunchKernelGGL(fork_deal_kernel<16>, grid, dim3(kThreads), (size_t)n_b * 4, st, table, lens, source, free_list, n_b, max_blocks, n_blocks, shift,
+                       moves, n_moves, granted);
+  return hipGetLastError();
+}
+
+size_t compact_scratch_bytes(int n_blocks) { return 64 + 4 * (size_t)div_up(n_blocks, 32) * sizeof(uint32_t); }
+
+hipError_t launch_paged_compact(int32_t* table, const int32_t* lens, int32_t* free_list, int n_b, int max_blocks, int n_blocks, int shift,
+                                int32_t* moves, int n_moves, int32_t* extent, void* workspace, hipStream_t st) {
+  const int words = div_up(n_blocks, 32);
+  CompactScratch w;
+  w.head = static_cast<int32_t*>(workspace);
+  w.free = reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(workspace) + 64);
+  w.used = w.free + words;
+  w.free_before = w.used + words;
+  w.used_before = w.free_before + words;
+  const dim3 blocks((unsigned)div_up(n_blocks, kThreads)), threads(kThreads);
+  const int across = div_up(max_blocks, kThreads * 4);
+  const dim3 entries((unsigned)n_b, (unsigned)(across < 64 ? across : 64));
+  hipError_t e;
+#define CKV_STEP(name, kernel, grid, block, ...)                        \
+  {                                                                     \
+    ScopedTimer t(name, st);                                            \
+    hipLaunchKernelGGL(kernel, grid, block, 0, st, __VA_ARGS__);        \
+  }                                                                     \
+  e = hipGetLastError();                                                \
+  if (e != hipSuccess) return e
+  CKV_STEP("compact_free", compact_free_kernel, blocks, threads, free_list, n_blocks, w, extent);
+  CKV_STEP("compact_used", compact_used_kernel, entries, threads, table, lens, max_blocks, n_blocks, shift, w);
+  CKV_STEP("compact_scan", compact_scan_kernel, dim3(1), dim3(kScanThreads), words, n_moves, w);
+  CKV_STEP("compact_blocks", compact_blocks_kernel, blocks, threads, free_list, n_blocks, w, moves, n_moves, extent);
+  CKV_STEP("compact_rename", compact_rename_kernel, entries, threads, table, lens, max_blocks, n_blocks, shift, w, moves);
+#undef CKV_STEP
+  return hipSuccess;
+}
+
+hipError_t launch_paged_copy(const int32_t* moves, int n_moves, void* K, void* V, int32_t* deg, void* bounds, int32_t* mass, int n_blocks, int heads,
+                             int block_size, int row_bytes, hipStream_t st) {
+  if (n_moves == 0) return hipSuccess;
+  ScopedTimer t("paged_copy", st);
+  const int pieces = heads * block_size * (row_bytes / 16);
+  const int group = pieces < kPieces ? kPieces / pieces : 1, parts = div_up(pieces, kPieces);
+  hipLaunchKernelGGL(paged_copy_kernel, dim3((unsigned)(div_up(n_moves, group) * parts)), dim3(kThreads), 0, st, moves, n_moves,
+                     static_cast<unsigned char*>(K), static_cast<unsigned char*>(V), deg, static_cast<unsigned char*>(bounds), mass, n_blocks, pieces,
+                     heads * block_size, heads, heads * 2 * (row_bytes / 16), group, parts);
+  return hipGetLastError();
+}
+
+}  // namespace ckv
