@@ -20,7 +20,7 @@ constexpr int kRows = 128;               // query rows of a workgroup
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr float kSlack = 8.f;            // how far (log2) a logit may exceed the reference before the sums are rescaled
 
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;   // kinds of instructions, for the order that the compiler is asked for
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 struct ChunkArgs {
@@ -65,8 +65,18 @@ struct Tile {
 __device__ __forceinline__ void to_lds16(const void* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
+// the same from a base that all lanes share
+__device__ __forceinline__ void to_lds16(const void* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// x, as something that the compiler knows nothing of: what a rare path works out from it is not kept in registers for it
+__device__ __forceinline__ int unknown(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // op over a lane and its partner 32 away
@@ -76,7 +86,7 @@ __device__ __forceinline__ float with_partner(float x, Op&& op) {
   return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <typename T, int D>
+template <typename T, int D, bool DEG>
 __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   using L = Tile<T, D>;
   constexpr int SUB = L::SUB, DT = D / 32;
@@ -130,6 +140,21 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     for (int s = 0; s < QP; ++s) qf[s] = *reinterpret_cast<const uint4*>(qr + (2 * s + half) * 16);
   }
 
+  // ---- where a lane reads in a tile: its keys' pieces (row col), and its values (bf16: of a 4 x 16 block that lanes 16 g ..
+  // 16 g + 15 read transposed, tokens 4 half + .., channels 16 (g & 1) + ..; fp32: token 4 half, channel col).  The tile's other
+  // rows are a constant away.
+  using LdsAt = const __attribute__((address_space(3))) unsigned char*;
+  const LdsAt lds_tiles = (LdsAt)s_tiles;
+  int k_at[QP], v_at[DT];
+#pragma unroll
+  for (int st = 0; st < QP; ++st) k_at[st] = col * L::RB + L::k_slot(col, 2 * st + half) * 16;
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    const int r = L::BF16 ? 4 * half + ((lane & 15) >> 2) : 4 * half;
+    const int at = L::BF16 ? 64 * d + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) : 128 * d + 4 * col;
+    v_at[d] = L::BYTES + r * L::RB + L::v_slot(r, at >> 4) * 16 + (at & 15);
+  }
+
   f32x16 acc[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -137,37 +162,47 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   float ref = -INFINITY, sum = 0.f;
 
-  // ---- staging.  A lane's rows of a tile: ROWS_PER_LOAD rows a load, wave w's loads one behind the other.
-  const int r0 = wave * L::LOADS * L::ROWS_PER_LOAD + lane / L::PIECES, slot_in_row = lane % L::PIECES;
+  // ---- staging: a load takes ROWS_PER_LOAD rows, wave w's loads one behind the other.  A lane holds the table's entry of one of the
+  // tile's tokens, asked for a tile ahead.  Where a load's rows lie in one block, their place is a matter of scalars.
+  constexpr int PER = L::ROWS_PER_LOAD, RB_SHIFT = __builtin_ctz(L::RB);
+  const int r_lane = lane / L::PIECES, slot_in_row = lane % L::PIECES;
+  const bool whole_loads = (1 << shift) >= PER;
   auto entry = [&](int t) { return table[min(t, seen - 1) >> shift]; };
-  auto pool_row = [&](int e, int t) -> int64_t {        // (an entry outside the pool: row 0, masked)
-    return (unsigned)e < (unsigned)a.paged.n_blocks ? (((int64_t)e * a.heads + kvh) << shift) + (min(t, seen - 1) & mask) : 0;
+  auto pool_row = [&](int e, int t) {                    // (an entry outside the pool: the pool's first rows, masked)
+    return (unsigned)e < (unsigned)a.paged.n_blocks ? ((e * a.heads + kvh) << shift) + (t & mask) : 0;
   };
-  int ent[L::LOADS], ent_d = 0;
-  auto ask_entries = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) ent[i] = entry(tile * L::TILE + r0 + i * L::ROWS_PER_LOAD);
-    if (wave == kWaves - 1) ent_d = entry(tile * L::TILE + (lane & (L::TILE - 1)));
-  };
+  int ent = 0;
+  auto ask_entries = [&](int tile) { ent = entry(tile * L::TILE + (lane & (L::TILE - 1))); };
   const uint32_t lds0 = lds_address(s_tiles);
   int dg = 1;
-  auto request = [&](int tile, int buf) {
+  auto request = [&](int tile, int buf) __attribute__((always_inline)) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)buf * 2 * L::BYTES + (uint32_t)wave * L::LOADS * 1024);
+    const int first_row = __builtin_amdgcn_readfirstlane(wave * L::LOADS * PER);
+    if (whole_loads) {
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int r = r0 + i * L::ROWS_PER_LOAD;
-      const int64_t at = pool_row(ent[i], tile * L::TILE + r) * L::RB;
-      to_lds16(a.K + at + L::k_slot(r, slot_in_row) * 16, to + i * 1024);
-      to_lds16(a.V + at + L::v_slot(r, slot_in_row) * 16, to + L::BYTES + i * 1024);
+      for (int i = 0; i < L::LOADS; ++i) {
+        const int r = first_row + i * PER;
+        const uint64_t at = (uint64_t)(uint32_t)pool_row(__builtin_amdgcn_readlane(ent, r), tile * L::TILE + r) << RB_SHIFT;
+        to_lds16(a.K + at, (uint32_t)(r_lane * L::RB + L::k_slot(r + r_lane, slot_in_row) * 16), to + i * 1024);
+        to_lds16(a.V + at, (uint32_t)(r_lane * L::RB + L::v_slot(r + r_lane, slot_in_row) * 16), to + L::BYTES + i * 1024);
+      }
+    } else {
+      const int l = unknown(lane);
+      for (int i = 0; i < L::LOADS; ++i) {
+        const int r = first_row + i * PER + l / L::PIECES;
+        const uint64_t at = (uint64_t)(uint32_t)pool_row(__shfl(ent, r), tile * L::TILE + r) << RB_SHIFT;
+        to_lds16(a.K + at + L::k_slot(r, l % L::PIECES) * 16, to + i * 1024);
+        to_lds16(a.V + at + L::v_slot(r, l % L::PIECES) * 16, to + L::BYTES + i * 1024);
+      }
     }
-    if (wave == kWaves - 1 && a.deg) dg = a.deg[pool_row(ent_d, tile * L::TILE + (lane & (L::TILE - 1)))];
+    if (DEG && wave == kWaves - 1) dg = a.deg[pool_row(ent, tile * L::TILE + (lane & (L::TILE - 1)))];
   };
   // what the last wave says of a tile's tokens: ln N / scale of each (the product's first addend), and which count
   auto describe = [&](int tile, int buf, int e) {
     if (wave == kWaves - 1) {
       const int i = lane & (L::TILE - 1);
       const bool ok = tile * L::TILE + i < seen && (unsigned)e < (unsigned)a.paged.n_blocks && dg > 0;
-      if (a.deg && lane < L::TILE) s_bias[buf][i] = ok ? __log2f((float)dg) / a.c : 0.f;
+      if (DEG && lane < L::TILE) s_bias[buf][i] = ok ? __log2f((float)dg) / a.c : 0.f;
       const uint64_t valid = __ballot(ok);
       if (lane == 0) s_valid[buf] = valid;
     }
@@ -176,7 +211,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   if (tile0 < tile1) {
     ask_entries(tile0);
     request(tile0, 0);
-    const int e0 = ent_d;
+    const int e0 = ent;
     ask_entries(tile0 + 1);
     describe(tile0, 0, e0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -185,13 +220,12 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   for (int tile = tile0; tile < tile1; ++tile) {
     const int buf = (tile - tile0) & 1, t0 = tile * L::TILE;
     const bool more = tile + 1 < tile1;
-    const int e_next = ent_d;
+    const int e_next = ent;
     if (more) {
       request(tile + 1, buf ^ 1);
       ask_entries(tile + 2);
     }
-    unsigned char* sk = s_tiles + buf * 2 * L::BYTES;
-    unsigned char* sv = sk + L::BYTES;
+    const LdsAt tile_at = lds_tiles + buf * 2 * L::BYTES;
     const uint64_t valid = ((uint64_t)__builtin_amdgcn_readfirstlane((int)(s_valid[buf] >> 32)) << 32) |
                            (uint32_t)__builtin_amdgcn_readfirstlane((int)s_valid[buf]);
     const bool edge = t0 + L::TILE - 1 > all_see || valid != ~0ull;
@@ -201,9 +235,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
       // that do not count become zero; so do infinities and NaN, which are added to the rows that see them afterwards.
       if (tid == 0) s_odd = 0;
       __syncthreads();
-      for (int p = tid; p < L::TILE * L::PIECES; p += kThreads) {
+      for (int p = unknown(tid); p < L::TILE * L::PIECES; p += kThreads) {
         const int r = p / L::PIECES;
-        uint4* at = reinterpret_cast<uint4*>(sv) + p;
+        uint4* at = reinterpret_cast<uint4*>(s_tiles + (2 * buf + 1) * L::BYTES) + p;
         uint4 u = *at;
         uint32_t* w = reinterpret_cast<uint32_t*>(&u);
         bool changed = false, strange = false;
@@ -233,22 +267,19 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
       // ---- S^T: lane (col, half), register i: token 8 (i / 4) + 4 half + i % 4 of its 32
       f32x16 s[SUB];
 #pragma unroll
-      for (int u = 0; u < SUB; ++u) {
-        if (a.deg) {
+      for (int u = 0; u < SUB; ++u)
 #pragma unroll
-          for (int i4 = 0; i4 < 4; ++i4) {
-            const f32x4 v = *reinterpret_cast<const f32x4*>(&s_bias[buf][u * 32 + 8 * i4 + 4 * half]);
+        for (int i4 = 0; i4 < 4; ++i4) {
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
+          if (DEG) v = *reinterpret_cast<const f32x4*>(&s_bias[buf][u * 32 + 8 * i4 + 4 * half]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[u][4 * i4 + i] = v[i];
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+          for (int i = 0; i < 4; ++i) s[u][4 * i4 + i] = v[i];
         }
-        const int r = u * 32 + col;
 #pragma unroll
-        for (int st = 0; st < QP; ++st) {
-          const uint4 kf = *reinterpret_cast<const uint4*>(sk + r * L::RB + L::k_slot(r, 2 * st + half) * 16);
+      for (int st = 0; st < QP; ++st)
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+          const u32x4 kf = *(const __attribute__((address_space(3))) u32x4*)(tile_at + k_at[st] + u * 32 * L::RB);
           if constexpr (L::BF16) {
             s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[st]), s[u], 0, 0, 0);
           } else {
@@ -257,14 +288,24 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
             for (int j = 0; j < 4; ++j) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[j], qq[j], s[u], 0, 0, 0);
           }
         }
+      if constexpr (L::BF16) {
+        __builtin_amdgcn_sched_group_barrier(kDsRead, (DEG ? 8 : 0) + QP, 0);
+#pragma unroll
+        for (int i = 0; i < QP; ++i) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMfma, QP, 0);
       }
       if (edge) {
+        const int lim = unknown(limit - t0 - 4 * half);
+        const uint64_t ok = valid >> (4 * half);
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int j = u * 32 + 8 * (i >> 2) + (i & 3) + 4 * half;
-            if (t0 + j > limit || !((valid >> j) & 1)) s[u][i] = -INFINITY;
+            const int j = u * 32 + 8 * (i >> 2) + (i & 3);
+            if (j > lim || !((ok >> j) & 1)) s[u][i] = -INFINITY;
           }
       }
       // ---- softmax against a reference that follows the maximum once it is 2^8 below it
@@ -302,28 +343,34 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-              // lanes 16 g .. 16 g + 15 read a 4 x 16 block: tokens 4 half + .., channels 16 (g & 1) + ..
               union { s16x4 h[2]; bf16x8 v; } vt;
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int r = u * 32 + 16 * k + 8 * e + 4 * half + ((lane & 15) >> 2);
-                const int at = 64 * d + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+              for (int e = 0; e < 2; ++e)
                 vt.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(sv + r * L::RB + L::v_slot(r, at >> 4) * 16 + (at & 8)));
-              }
+                    (__attribute__((address_space(3))) s16x4*)(tile_at + v_at[d] + (u * 32 + 16 * k + 8 * e) * L::RB));
               acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt.v, p.v, acc[d], 0, 0, 0);
             }
           }
+        __builtin_amdgcn_sched_group_barrier(kValu, 24, 1);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2 * DT, 1);
+#pragma unroll
+        for (int g = 0; g < 2 * SUB - 1; ++g)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+            __builtin_amdgcn_sched_group_barrier(kValu, 24 / DT, 1);
+          }
+        __builtin_amdgcn_sched_group_barrier(kMfma, DT, 1);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float w = exp2_raw(fmaf(s[0][i], a.c, -base));
           sum += w;
-          const int r = 8 * (i >> 2) + 4 * half + (i & 3);
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
-            const int at = 128 * d + 4 * col;
-            const float v = *reinterpret_cast<const float*>(sv + r * L::RB + L::v_slot(r, at >> 4) * 16 + (at & 15));
+            // (rows 8 i + 4 half + .. of a d have their slots alike)
+            const float v = *(const __attribute__((address_space(3))) float*)(tile_at + v_at[d] + (8 * (i >> 2) + (i & 3)) * L::RB);
             acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w, acc[d], 0, 0, 0);
           }
         }
@@ -333,7 +380,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
         const int j = __builtin_ctzll(odd);
         odd &= odd - 1;
         const int t = t0 + j;
-        const unsigned char* vr = a.V + pool_row(entry(t), t) * L::RB;
+        const unsigned char* vr = a.V + ((uint64_t)(uint32_t)pool_row(entry(t), t) << RB_SHIFT);
         if (t <= limit) {
 #pragma unroll
           for (int d = 0; d < DT; ++d)
@@ -477,15 +524,15 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
   a.o_part = a.ml_part + (rows * cut.splits * 2 + 3) / 4 * 4;
   const dim3 grid((unsigned)((int64_t)cut.slots * c.heads * cut.splits));
   hipError_t e = hipErrorInvalidValue;
-#define CKV_CHUNK(T, D)                                                                                               \
+#define CKV_CHUNK_DEG(T, D, DEG)                                                                                             \
   do {                                                                                                                \
     static KernelSetup setup;                                                                                         \
     constexpr size_t lds = 4 * Tile<T, D>::BYTES;                                                                     \
-    e = kernel_setup(reinterpret_cast<const void*>(&chunk_attn_kernel<T, D>), lds, setup);                            \
+    e = kernel_setup(reinterpret_cast<const void*>(&chunk_attn_kernel<T, D, DEG>), lds, setup);                         \
     if (e != hipSuccess) return e;                                                                                    \
     {                                                                                                                 \
       ScopedTimer t("chunk_attn", st);                                                                                \
-      hipLaunchKernelGGL((chunk_attn_kernel<T, D>), grid, dim3(kThreads), lds, st, a);                                \
+      hipLaunchKernelGGL((chunk_attn_kernel<T, D, DEG>), grid, dim3(kThreads), lds, st, a);                           \
     }                                                                                                                 \
     e = hipGetLastError();                                                                                            \
     if (e == hipSuccess && cut.splits > 1) {                                                                          \
@@ -494,6 +541,11 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
                          cut.splits, rows, c.q_heads, c.starts, c.n_b, c.n, c.o, c.o_dtype);                          \
       e = hipGetLastError();                                                                                          \
     }                                                                                                                 \
+  } while (0)
+#define CKV_CHUNK(T, D)                    \
+  do {                                     \
+    if (c.deg) CKV_CHUNK_DEG(T, D, true);  \
+    else CKV_CHUNK_DEG(T, D, false);       \
   } while (0)
   if (dtype == CKV_BF16) {
     if (dim == 64) CKV_CHUNK(__bf16, 64);
@@ -504,6 +556,7 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
     else if (dim == 128) CKV_CHUNK(float, 128);
   }
 #undef CKV_CHUNK
+#undef CKV_CHUNK_DEG
   return e;
 }
 
