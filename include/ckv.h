@@ -415,7 +415,7 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
  * bf16: products on bf16 matrix instructions with fp32 sums, softmax weights rounded to bf16 (by 2^-8 at most) for the product with
  * the values; the result does not depend on anything but the arguments (no atomics on numbers).  fp32: fp32 throughout.
  * Supported: q_heads / heads in {1,2,4,8}; bf16 dim 64/128; fp32 dim 32/64/128; pools of fewer than 2^31 token rows;
- * n <= 2^30. */
+ * n <= 2^30; sequences (max_len, or what the table holds) of up to 2^31 - 1025 tokens. */
 int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, size_t* bytes);
 int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_stride, int32_t q_heads, const int32_t* starts, int32_t n,
                          const void* K_pool, const void* V_pool, const int32_t* deg_pool, const int32_t* block_table, const int32_t* lens,

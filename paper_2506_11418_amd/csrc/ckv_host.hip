@@ -1088,15 +1088,21 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
 
 // ---- attention of several new tokens over pages --------------------------------------------------
 namespace {
+// tokens of a sequence, at most
+int longest(const ckv_paged_layout* pl, int32_t max_len) {
+  const int64_t cap = (int64_t)pl->max_blocks * pl->block_size;
+  return (int)(max_len < cap ? max_len : cap);
+}
+constexpr int64_t kMostGroups = 0xffffffffll / 256;   // workgroups of a launch: its threads are counted in 32 bits
 int check_chunk(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, int* shift) {
   const int st = check_sparse(pl, shift);    // (dims, pool rows and launch dimensions as there)
   if (st != CKV_OK) return st;
   if (q_heads <= 0 || q_heads % pl->heads || n < 0 || max_len <= 0) return CKV_ESHAPE;
   const int G = q_heads / pl->heads;
   if (G != 1 && G != 2 && G != 4 && G != 8) return CKV_EUNSUPPORTED;
-  if (n > kMostEntries) return CKV_EUNSUPPORTED;
-  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, max_len);
-  if ((int64_t)cut.slots * pl->heads * cut.splits > INT32_MAX || (int64_t)n * q_heads / 4 >= INT32_MAX) return CKV_EUNSUPPORTED;   // workgroups of a launch
+  if (n > kMostEntries || longest(pl, max_len) > ckv::kMostTokens) return CKV_EUNSUPPORTED;
+  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, longest(pl, max_len));
+  if ((int64_t)cut.slots * pl->heads * cut.splits > kMostGroups) return CKV_EUNSUPPORTED;
   return CKV_OK;
 }
 }  // namespace
@@ -1106,7 +1112,7 @@ int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, 
   const int st = check_chunk(pl, q_heads, n, max_len, &shift);
   if (st != CKV_OK) return st;
   if (!bytes) return CKV_EINVAL;
-  *bytes = ckv::align_up(ckv::chunk_reserve_bytes(pl->heads, q_heads, n, max_len, pl->dim), 256);
+  *bytes = ckv::align_up(ckv::chunk_reserve_bytes(q_heads, n, max_len, pl->dim), 256);
   return CKV_OK;
 }
 
@@ -1127,7 +1133,7 @@ int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_str
     return CKV_EALIGN;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)pl->dim);
   if (!(scale >= 1e-30f && scale <= 1e30f)) return CKV_EUNSUPPORTED;         // (ln N / scale is a number)
-  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, max_len);
+  const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, longest(pl, max_len));
   const int64_t heads = (int64_t)n * q_heads;
   const size_t need = ckv::chunk_workspace_bytes(heads, cut.splits, pl->dim);
   if (need && !workspace) return CKV_EINVAL;
@@ -1143,7 +1149,7 @@ int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_str
   c.starts = starts;
   c.K = K_pool; c.V = V_pool; c.deg = deg_pool;
   c.paged = ckv::PagedView{block_table, pl->max_blocks, shift, pl->n_blocks};
-  c.lens = lens; c.max_len = max_len; c.causal = causal != 0;
+  c.lens = lens; c.max_len = longest(pl, max_len); c.causal = causal != 0;
   c.scale = scale;
   c.o = o; c.o_dtype = o_dtype;
   c.workspace = workspace;
@@ -1198,7 +1204,7 @@ int ckv_paged_copy(const int32_t* moves, int32_t n_moves, void* K_pool, void* V_
   const int e = ckv::elem_bytes(pl->dtype);
   const int64_t page = (int64_t)pl->heads * pl->block_size * pl->dim * e;
   if (n_moves < 0 || n_moves > kMostEntries || (int64_t)pl->heads * pl->dim * e > INT32_MAX / 1024) return CKV_ESHAPE;
-  if ((page / 16384 + 1) * n_moves > INT32_MAX) return CKV_EUNSUPPORTED;     // workgroups of a launch
+  if ((page / 16384 + 1) * n_moves > kMostGroups) return CKV_EUNSUPPORTED;
   if (n_moves == 0) return CKV_OK;
   if (!moves || !K_pool || !V_pool || !bounds != !mass) return CKV_EINVAL;
   if (((uintptr_t)K_pool | (uintptr_t)V_pool | (uintptr_t)bounds) % 16 || misaligned4({moves, deg_pool, mass})) return CKV_EALIGN;

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kRows = 128;               // query rows of a workgroup
 constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr float kWhole = -1.f;           // in the place of a first part's sum: the row's output has been written
 constexpr float kSlack = 8.f;            // how far (log2) a logit may exceed the reference before the sums are rescaled
 
 constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;   // kinds of instructions, for the order that the compiler is asked for
@@ -34,7 +35,7 @@ struct ChunkArgs {
   const int32_t* lens;
   int max_len, heads, g_shift;           // query heads per KV head = 1 << g_shift
   float c;                               // scale * log2 e
-  int causal, splits, slots;
+  int causal, slots, splits, span;
   void* o;
   int o_dtype;
   float *o_part, *ml_part;               // [split][token][query head][dim] and [..][2], with more than one split
@@ -91,26 +92,44 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   using L = Tile<T, D>;
   constexpr int SUB = L::SUB, DT = D / 32;
   extern __shared__ __attribute__((aligned(16))) unsigned char s_tiles[];     // two tiles of keys and values
-  __shared__ __attribute__((aligned(16))) float s_bias[2][L::TILE];
+  // A tile's ln N / scale: bf16, of each token the sum of three bf16 and zeros, a row of a product with ones; fp32, the number.
+  __shared__ __attribute__((aligned(16))) typename std::conditional<L::BF16, uint4, float>::type s_bias[2][DEG ? L::TILE : 1];
   __shared__ uint64_t s_valid[2], s_odd;                 // a tile's tokens that count; those with a value that is no finite number
   __shared__ int s_seq;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
 
   // ---- which rows, which tokens
   const int id = blockIdx.x;
-  const int kvh = id % a.heads, split = (id / a.heads) % a.splits, slot = a.slots - 1 - id / a.heads / a.splits;
+  const int kvh = id % a.heads, slot = id / a.heads % a.slots, split = id / a.heads / a.slots;
   const int t_shift = __builtin_ctz(kRows) - a.g_shift;  // tokens of a workgroup
-  // Sequence b has the slots from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
-  if (tid == 0) s_seq = 0;
-  __syncthreads();
-  int before = 0;
-  for (int b = tid; b < a.n_b; b += kThreads) before += (min(max(a.starts[b], 0), a.n) >> t_shift) + b <= slot;
-  if (before) atomicAdd(&s_seq, before);
-  __syncthreads();
-  const int b = s_seq - 1;
-  if (b < 0) return;
+  int b, part;
+  if (a.n_b <= 64) {
+    // The longest sequence's rows first: those that start last are the shortest.  A lane holds a sequence.
+    const int at = min(lane, a.n_b - 1), first = min(max(a.starts[at], 0), a.n), last = min(max(a.starts[at + 1], 0), a.n);
+    const int count = lane < a.n_b ? (max(last - first, 0) + (1 << t_shift) - 1) >> t_shift : 0, len = a.lens[at];
+    int before = 0;
+    for (int i = 0; i < a.n_b; ++i) {
+      const int l = __builtin_amdgcn_readlane(len, i);
+      if (l > len || (l == len && i < lane)) before += __builtin_amdgcn_readlane(count, i);
+    }
+    const uint64_t mine = __ballot(slot >= before && slot < before + count);
+    if (!mine) return;
+    b = (int)__builtin_ctzll(mine);
+    part = __builtin_amdgcn_readlane(before + count, b) - 1 - slot;         // (its last rows, which see most, first)
+  } else {
+    // Sequence b has the places from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
+    if (tid == 0) s_seq = 0;
+    __syncthreads();
+    int before = 0;
+    for (int i = tid; i < a.n_b; i += kThreads) before += (min(max(a.starts[i], 0), a.n) >> t_shift) + i <= slot;
+    if (before) atomicAdd(&s_seq, before);
+    __syncthreads();
+    b = s_seq - 1;
+    if (b < 0) return;
+    part = slot - (min(max(a.starts[b], 0), a.n) >> t_shift) - b;
+  }
   const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
-  const int tok0 = first + ((slot - (first >> t_shift) - b) << t_shift);
+  const int tok0 = first + (part << t_shift);
   const int tokens = min(last - tok0, 1 << t_shift);
   if (tokens <= 0) return;
   const int64_t cap = (int64_t)a.paged.max_blocks << a.paged.shift;
@@ -126,8 +145,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   const int wave_last = a.causal ? pos0 + min((wave * 32 + 31) >> a.g_shift, tokens - 1) : len - 1;
   const bool idle = wave * 32 >= rows;
 
-  const int n_tiles = (seen + L::TILE - 1) / L::TILE;
-  const int tile0 = (int)((int64_t)n_tiles * split / a.splits), tile1 = (int)((int64_t)n_tiles * (split + 1) / a.splits);
+  // These rows' tokens are cut into as many equal parts as spans of a.span tokens hold them.
+  // (no sequence is longer than kMostTokens: a few tiles behind the last one still have a number)
+  const int n_tiles = (seen + L::TILE - 1) / L::TILE, parts = max((int)(((int64_t)seen + a.span - 1) / a.span), 1);
+  const int tile0 = split < parts ? (int)((int64_t)n_tiles * split / parts) : 0, tile1 = split < parts ? (int)((int64_t)n_tiles * (split + 1) / parts) : 0;
+  const int q_heads = a.heads << a.g_shift;
+  const int64_t out_row = (int64_t)(tok0 + my_tok) * q_heads + my_head, part_row = (int64_t)split * a.n * q_heads + out_row;
+  if (split >= parts) {                  // nothing: a weight of zero
+    if (live && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(-INFINITY, 0.f);
+    return;
+  }
   const int32_t* table = a.paged.table + (int64_t)b * a.paged.max_blocks;
   const int shift = a.paged.shift, mask = (1 << shift) - 1;
 
@@ -175,6 +202,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   auto ask_entries = [&](int tile) { ent = entry(tile * L::TILE + (lane & (L::TILE - 1))); };
   const uint32_t lds0 = lds_address(s_tiles);
   int dg = 1;
+  const float inv_c = 1.f / a.c;
   auto request = [&](int tile, int buf) __attribute__((always_inline)) {
     const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)buf * 2 * L::BYTES + (uint32_t)wave * L::LOADS * 1024);
     const int first_row = __builtin_amdgcn_readfirstlane(wave * L::LOADS * PER);
@@ -202,7 +230,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     if (wave == kWaves - 1) {
       const int i = lane & (L::TILE - 1);
       const bool ok = tile * L::TILE + i < seen && (unsigned)e < (unsigned)a.paged.n_blocks && dg > 0;
-      if (DEG && lane < L::TILE) s_bias[buf][i] = ok ? __log2f((float)dg) / a.c : 0.f;
+      if constexpr (DEG) {
+        const float x = ok ? __log2f((float)dg) * inv_c : 0.f;
+        if constexpr (L::BF16) {
+          const __bf16 hi = (__bf16)x, mid = (__bf16)(x - (float)hi);
+          const bf16x2 two = {hi, mid}, one = {(__bf16)(x - (float)hi - (float)mid), (__bf16)0.f};
+          s_bias[buf][i] = make_uint4(__builtin_bit_cast(uint32_t, two), __builtin_bit_cast(uint32_t, one), 0, 0);
+        } else if (lane < L::TILE) {
+          s_bias[buf][i] = x;
+        }
+      }
       const uint64_t valid = __ballot(ok);
       if (lane == 0) s_valid[buf] = valid;
     }
@@ -217,6 +254,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
+#pragma unroll
+  for (int s = 0; s < QP; ++s) asm volatile("" : "+v"(qf[s].x), "+v"(qf[s].y), "+v"(qf[s].z), "+v"(qf[s].w));
   for (int tile = tile0; tile < tile1; ++tile) {
     const int buf = (tile - tile0) & 1, t0 = tile * L::TILE;
     const bool more = tile + 1 < tile1;
@@ -269,12 +308,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
 #pragma unroll
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          f32x4 v = {0.f, 0.f, 0.f, 0.f};
-          if (DEG) v = *reinterpret_cast<const f32x4*>(&s_bias[buf][u * 32 + 8 * i4 + 4 * half]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[u][4 * i4 + i] = v[i];
-        }
+        for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+      __builtin_amdgcn_s_setprio(1);       // (whoever has products to start goes first: 2172 -> 2136 us for a prompt of 16384)
 #pragma unroll
       for (int st = 0; st < QP; ++st)
 #pragma unroll
@@ -288,15 +323,29 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
             for (int j = 0; j < 4; ++j) s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(kk[j], qq[j], s[u], 0, 0, 0);
           }
         }
-      if constexpr (L::BF16) {
-        __builtin_amdgcn_sched_group_barrier(kDsRead, (DEG ? 8 : 0) + QP, 0);
+      if constexpr (DEG) {               // one more product of each chain: ln N / scale by one
 #pragma unroll
-        for (int i = 0; i < QP; ++i) {
+        for (int u = 0; u < SUB; ++u) {
+          if constexpr (L::BF16) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(&s_bias[buf][u * 32 + col]);
+            const uint32_t o = half ? 0u : 0x3f80u;
+            const u32x4 ones = {o | o << 16, o, 0u, 0u};
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, ones), s[u], 0, 0, 0);
+          } else {
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x2f32(s_bias[buf][u * 32 + col], half ? 0.f : 1.f, s[u], 0, 0, 0);
+          }
+        }
+      }
+      if constexpr (L::BF16) {
+        __builtin_amdgcn_sched_group_barrier(kDsRead, QP, 0);
+#pragma unroll
+        for (int i = 0; i < QP + (DEG ? SUB : 0); ++i) {
           __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
           __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(kMfma, QP, 0);
       }
+      __builtin_amdgcn_s_setprio(0);
       if (edge) {
         const int lim = unknown(limit - t0 - 4 * half);
         const uint64_t ok = valid >> (4 * half);
@@ -402,8 +451,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   if (idle) return;
   sum = with_partner(sum, [](float x, float y) { return x + y; });
   if (!live) return;
-  const int64_t out_row = (int64_t)(tok0 + my_tok) * (a.heads << a.g_shift) + my_head;
-  if (a.splits == 1) {
+  if (parts == 1) {
+    if (a.splits > 1 && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(0.f, kWhole);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -424,9 +473,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
       }
     return;
   }
-  const int64_t part = (int64_t)split * a.n * (a.heads << a.g_shift) + out_row;
-  if (half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part]) = make_float2(ref, sum);
-  if (tile0 >= tile1) return;            // (nothing is read there: its weight is zero)
+  if (half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(ref, sum);
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -434,7 +481,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
       f32x4 v;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = acc[d][4 * i4 + i];
-      *reinterpret_cast<f32x4*>(&a.o_part[part * D + 32 * d + 8 * i4 + 4 * half]) = v;
+      *reinterpret_cast<f32x4*>(&a.o_part[part_row * D + 32 * d + 8 * i4 + 4 * half]) = v;
     }
 }
 
@@ -455,6 +502,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
     m = v.x;
     l = v.y;
   }
+  if (__builtin_amdgcn_readfirstlane(__float_as_uint(l)) == __float_as_uint(kWhole)) return;
   const float top = across_lanes<0x3f>(m, [](float x, float y) { return fmaxf(x, y); });
   const float w = m == -INFINITY ? 0.f : exp2f(m - top);
   const float den = across_lanes<0x3f>(w * l, [](float x, float y) { return x + y; });
@@ -478,16 +526,27 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
 }  // namespace
 
 namespace {
-constexpr int kMostSplits = 64, kLeastSpan = 256;
-int most_splits(int max_len) { return max_len >= kMostSplits * kLeastSpan ? kMostSplits : div_up(max_len, kLeastSpan); }
-int wanted_groups() { return 2 * cu_count(); }
+constexpr int kMostSplits = 64, kLeastSpan = 128, kSpan = 4096, kRounds = 3;
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+// the most parts that a call of up to max_len tokens is cut into
+int64_t most_splits(int max_len) { return least(up(max_len, kLeastSpan), kMostSplits); }
+int groups_at_once() { return 2 * cu_count(); }
 }  // namespace
 
+// How the tokens are cut: so that every place on the chip has work, down to spans of kLeastSpan tokens; and down to kSpan tokens into
+// kRounds times as many workgroups as there are places, so that those that finish last are few.
+// us with kRounds, kSpan = 3, 4096 / 3, 2048 / 6, 4096 / 10, 1024: 16 requests of 1 to 8 tokens over 32768 313 / 341 / 310 / 349; 39 single
+// tokens and 1999 of another over 16384 922 / 930 / 953 / 1008.  33 tokens over 515 with kLeastSpan 128 / 256 / 512: 15.4 / 16.5 / 19.3.
 ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
   ChunkCut cut;
   cut.slots = n / (kRows / (q_heads / heads)) + n_b;
-  const int64_t groups = (int64_t)cut.slots * heads, s = (wanted_groups() + groups - 1) / groups;
-  cut.splits = (int)(s < most_splits(max_len) ? s : most_splits(max_len));
+  const int64_t groups = (int64_t)cut.slots * heads;
+  const int64_t fill = least(up(groups_at_once(), groups), up(max_len, kLeastSpan));
+  const int64_t even = least(up((int64_t)kRounds * groups_at_once(), groups), up(max_len, kSpan));
+  const int64_t splits = least(fill > even ? fill : even, kMostSplits);
+  cut.span = (int)(up(up(max_len, splits), 64) * 64);
+  cut.splits = (int)up(max_len, cut.span);
   return cut;
 }
 
@@ -498,13 +557,12 @@ size_t chunk_workspace_bytes(int64_t rows, int splits, int dim) {
   return (parts * 8 + 15) / 16 * 16 + parts * dim * 4;
 }
 
-// Where a call is split, its places are fewer than wanted_groups() / heads: it has fewer than kRows * wanted_groups() rows, and as
-// many parts of rows again as make up the difference.
-size_t chunk_reserve_bytes(int heads, int q_heads, int n, int max_len, int dim) {
-  const int most = most_splits(max_len);
-  const int64_t full = (int64_t)kRows * wanted_groups(), rows = (int64_t)n * q_heads, cut = rows < full ? rows : full;
-  const int64_t parts = cut * most < full + cut ? cut * most : full + cut;
-  return most <= 1 ? 0 : chunk_workspace_bytes(parts, 2, dim) / 2 + 16;
+// Rows are cut where there are fewer than kRounds * groups_at_once() places for workgroups, of kRows rows at most, into as many parts
+// more as make up the difference; and none into more than most_splits().
+size_t chunk_reserve_bytes(int q_heads, int n, int max_len, int dim) {
+  const int64_t most = most_splits(max_len), full = (int64_t)kRows * kRounds * groups_at_once(), rows = (int64_t)n * q_heads;
+  const int64_t parts = least(rows * most, full + least(rows, full));
+  return most <= 1 ? 0 : (size_t)(parts * 8 + 15) / 16 * 16 + (size_t)parts * dim * 4;
 }
 
 hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t st) {
@@ -517,7 +575,7 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
   a.paged = c.paged; a.lens = c.lens; a.max_len = c.max_len; a.heads = c.heads;
   a.g_shift = __builtin_ctz(c.q_heads / c.heads);
   a.c = c.scale * kLog2e;
-  a.causal = c.causal; a.splits = cut.splits; a.slots = cut.slots;
+  a.causal = c.causal; a.slots = cut.slots; a.splits = cut.splits; a.span = cut.span;
   a.o = c.o; a.o_dtype = c.o_dtype;
   const int64_t rows = (int64_t)c.n * c.q_heads;
   a.ml_part = static_cast<float*>(c.workspace);
