@@ -135,7 +135,8 @@ def test_compact_refuses(kw, status):
 
 def test_compact_workspace():
     for n in (1, 31, 32, 33, 1000, 1 << 20):
-        assert 64 + n // 2 <= ckv.paged_compact_workspace(n) < 64 + n // 2 + 512
+        words = -(-n // 32)                  # a byte and four bits a block, and what is counted
+        assert 64 + 48 * words <= ckv.paged_compact_workspace(n) < 64 + 48 * words + 256
         assert _compact(blocks=n, bytes=ckv.paged_compact_workspace(n), extent=_p(2)) == -1      # (large enough: the overlap is found next)
     for n in (0, -5):
         with pytest.raises(ckv.CkvError):
