@@ -1102,7 +1102,7 @@ int check_chunk(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t 
   if (G != 1 && G != 2 && G != 4 && G != 8) return CKV_EUNSUPPORTED;
   if (n > kMostEntries || longest(pl, max_len) > ckv::kMostTokens) return CKV_EUNSUPPORTED;
   const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, longest(pl, max_len));
-  if ((int64_t)cut.slots * pl->heads * cut.splits > kMostGroups) return CKV_EUNSUPPORTED;
+  if ((cut.slots + (int64_t)cut.tail * (cut.splits - 1)) * pl->heads > kMostGroups) return CKV_EUNSUPPORTED;
   return CKV_OK;
 }
 }  // namespace
@@ -1112,7 +1112,7 @@ int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, 
   const int st = check_chunk(pl, q_heads, n, max_len, &shift);
   if (st != CKV_OK) return st;
   if (!bytes) return CKV_EINVAL;
-  *bytes = ckv::align_up(ckv::chunk_reserve_bytes(q_heads, n, max_len, pl->dim), 256);
+  *bytes = ckv::align_up(ckv::chunk_reserve_bytes(pl->heads, q_heads, n, max_len, pl->dim), 256);
   return CKV_OK;
 }
 
@@ -1135,7 +1135,7 @@ int ckv_paged_chunk_attn(const void* q, int64_t q_row_stride, int64_t q_head_str
   if (!(scale >= 1e-30f && scale <= 1e30f)) return CKV_EUNSUPPORTED;         // (ln N / scale is a number)
   const ckv::ChunkCut cut = ckv::chunk_cut(pl->batch, pl->heads, q_heads, n, longest(pl, max_len));
   const int64_t heads = (int64_t)n * q_heads;
-  const size_t need = ckv::chunk_workspace_bytes(heads, cut.splits, pl->dim);
+  const size_t need = ckv::chunk_workspace_bytes(cut, pl->heads, heads, pl->dim);
   if (need && !workspace) return CKV_EINVAL;
   if (workspace_bytes < need) return CKV_EWORKSPACE;
   const size_t row = (size_t)pl->dim * e, rows = (size_t)pl->n_blocks * pl->heads * pl->block_size, b4 = (size_t)pl->batch * 4;

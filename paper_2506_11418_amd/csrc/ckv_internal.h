@@ -262,11 +262,11 @@ struct ChunkCall {
   int o_dtype;
   void* workspace;
 };
-struct ChunkCut { int slots, splits, span; };   // places for workgroups' rows; parts that the tokens are cut into, of `span` tokens
+struct ChunkCut { int slots, splits, span, tail; };   // places for workgroups' rows; the last `tail` of them cut into parts of `span` tokens
 ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len);
-size_t chunk_workspace_bytes(int64_t rows, int splits, int dim);                                     // of this very call
+size_t chunk_workspace_bytes(const ChunkCut& cut, int heads, int64_t rows, int dim);                 // of this very call
 constexpr int kMostTokens = INT32_MAX - 1024;                             // of a sequence
-size_t chunk_reserve_bytes(int q_heads, int n, int max_len, int dim);     // enough for every call of up to that many tokens, any batch
+size_t chunk_reserve_bytes(int heads, int q_heads, int n, int max_len, int dim);   // enough for every call of up to that many tokens, any batch
 hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t st);
 
 // see k11_pages.hip

@@ -35,11 +35,53 @@ struct ChunkArgs {
   const int32_t* lens;
   int max_len, heads, g_shift;           // query heads per KV head = 1 << g_shift
   float c;                               // scale * log2 e
-  int causal, slots, splits, span;
+  int causal, slots, splits, span, tail;
   void* o;
   int o_dtype;
-  float *o_part, *ml_part;               // [split][token][query head][dim] and [..][2], with more than one split
+  float *o_part, *ml_part;               // [split][token][query head][dim] and [..][2], with more than one split;
+};                                       // where only a tail is cut, [place from the end][KV head][split][row]..
+
+// The rows of a place: tokens tok0 .. of sequence b.
+struct Rows {
+  int b, tok0, tokens, len, pos0, seen;  // pos0: position of the first of these tokens; seen: tokens that any of them sees
 };
+
+// Which rows the workgroup at `slot` has, of a batch of up to 64: the longest sequence's first, so that those that start last are the shortest,
+// and of a sequence the last ones, which see most.  A lane holds a sequence.  used: places that have rows.
+// back: count from the end of those (`slot` becomes the place).  All lanes of the wave take part.
+__device__ __forceinline__ bool in_order(const ChunkArgs& a, int t_shift, int lane, bool back, int& slot, int& used, int& b, int& part) {
+  const int at = min(lane, a.n_b - 1), first = min(max(a.starts[at], 0), a.n), last = min(max(a.starts[at + 1], 0), a.n);
+  const int count = lane < a.n_b ? (max(last - first, 0) + (1 << t_shift) - 1) >> t_shift : 0, len = a.lens[at];
+  int before = 0;
+  used = 0;
+  for (int i = 0; i < a.n_b; ++i) {
+    const int l = __builtin_amdgcn_readlane(len, i), c = __builtin_amdgcn_readlane(count, i);
+    if (l > len || (l == len && i < lane)) before += c;
+    used += c;
+  }
+  if (back) slot = used - 1 - slot;
+  const uint64_t mine = __ballot(slot >= before && slot < before + count);
+  if (!mine) return false;
+  b = (int)__builtin_ctzll(mine);
+  part = __builtin_amdgcn_readlane(before + count, b) - 1 - slot;
+  return true;
+}
+
+__device__ __forceinline__ bool rows_of(const ChunkArgs& a, int t_shift, int b, int part, Rows& r) {
+  const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
+  r.b = b;
+  r.tok0 = first + (part << t_shift);
+  r.tokens = min(last - r.tok0, 1 << t_shift);
+  if (part < 0 || r.tokens <= 0) return false;
+  const int64_t cap = (int64_t)a.paged.max_blocks << a.paged.shift;
+  r.len = (int)min((int64_t)min(max(a.lens[b], 0), a.max_len), cap);
+  r.pos0 = r.len - (last - r.tok0);
+  r.seen = a.causal ? max(min(r.pos0 + r.tokens, r.len), 0) : r.len;
+  return true;
+}
+
+// These rows' tokens are cut into as many equal parts as spans of a.span tokens hold them.
+__device__ __forceinline__ int parts_of(const ChunkArgs& a, int seen) { return max((int)(((int64_t)seen + a.span - 1) / a.span), 1); }
 
 // What a tile of the cache looks like for each type.  PIECES: 16-byte pieces of a row; TILE: tokens.
 template <typename T, int D>
@@ -98,26 +140,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ int s_seq;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
 
-  // ---- which rows, which tokens
-  const int id = blockIdx.x;
-  const int kvh = id % a.heads, slot = id / a.heads % a.slots, split = id / a.heads / a.slots;
+  // ---- which rows, which tokens: first every place's first part, then the others of the places that are cut
+  const int kvh = blockIdx.x % a.heads, place = blockIdx.x / a.heads;
   const int t_shift = __builtin_ctz(kRows) - a.g_shift;  // tokens of a workgroup
-  int b, part;
+  const int split = place < a.slots ? 0 : 1 + (place - a.slots) / a.tail;
+  int b, part, used = a.slots, slot = split ? a.tail - 1 - (place - a.slots) % a.tail : place;
   if (a.n_b <= 64) {
-    // The longest sequence's rows first: those that start last are the shortest.  A lane holds a sequence.
-    const int at = min(lane, a.n_b - 1), first = min(max(a.starts[at], 0), a.n), last = min(max(a.starts[at + 1], 0), a.n);
-    const int count = lane < a.n_b ? (max(last - first, 0) + (1 << t_shift) - 1) >> t_shift : 0, len = a.lens[at];
-    int before = 0;
-    for (int i = 0; i < a.n_b; ++i) {
-      const int l = __builtin_amdgcn_readlane(len, i);
-      if (l > len || (l == len && i < lane)) before += __builtin_amdgcn_readlane(count, i);
-    }
-    const uint64_t mine = __ballot(slot >= before && slot < before + count);
-    if (!mine) return;
-    b = (int)__builtin_ctzll(mine);
-    part = __builtin_amdgcn_readlane(before + count, b) - 1 - slot;         // (its last rows, which see most, first)
+    if (!in_order(a, t_shift, lane, split > 0, slot, used, b, part)) return;
   } else {
     // Sequence b has the places from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
+    if (split) slot = a.slots - 1 - slot;
     if (tid == 0) s_seq = 0;
     __syncthreads();
     int before = 0;
@@ -128,31 +160,28 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     if (b < 0) return;
     part = slot - (min(max(a.starts[b], 0), a.n) >> t_shift) - b;
   }
-  const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
-  const int tok0 = first + (part << t_shift);
-  const int tokens = min(last - tok0, 1 << t_shift);
-  if (tokens <= 0) return;
-  const int64_t cap = (int64_t)a.paged.max_blocks << a.paged.shift;
-  const int len = (int)min((int64_t)min(max(a.lens[b], 0), a.max_len), cap);
-  const int pos0 = len - (last - tok0);                  // position of the first of these tokens
+  Rows mine;
+  if (!rows_of(a, t_shift, b, part, mine)) return;
+  const int tok0 = mine.tok0, tokens = mine.tokens, len = mine.len, pos0 = mine.pos0, seen = mine.seen;
   const int rows = tokens << a.g_shift;
   const int row = wave * 32 + col;
   const bool live = row < rows;
   const int my_tok = min(row >> a.g_shift, tokens - 1), my_head = (kvh << a.g_shift) + (row & ((1 << a.g_shift) - 1));
   const int limit = a.causal ? pos0 + my_tok : len - 1;  // the last token that this row sees
-  const int seen = a.causal ? max(min(pos0 + tokens, len), 0) : len;          // tokens that any row sees
   const int all_see = a.causal ? pos0 : len - 1;         // the last one that every row sees
   const int wave_last = a.causal ? pos0 + min((wave * 32 + 31) >> a.g_shift, tokens - 1) : len - 1;
   const bool idle = wave * 32 >= rows;
 
-  // These rows' tokens are cut into as many equal parts as spans of a.span tokens hold them.
   // (no sequence is longer than kMostTokens: a few tiles behind the last one still have a number)
-  const int n_tiles = (seen + L::TILE - 1) / L::TILE, parts = max((int)(((int64_t)seen + a.span - 1) / a.span), 1);
+  const int from_end = used - 1 - slot;
+  const int n_tiles = (seen + L::TILE - 1) / L::TILE, parts = from_end < a.tail ? parts_of(a, seen) : 1;
   const int tile0 = split < parts ? (int)((int64_t)n_tiles * split / parts) : 0, tile1 = split < parts ? (int)((int64_t)n_tiles * (split + 1) / parts) : 0;
   const int q_heads = a.heads << a.g_shift;
-  const int64_t out_row = (int64_t)(tok0 + my_tok) * q_heads + my_head, part_row = (int64_t)split * a.n * q_heads + out_row;
+  const bool all_cut = a.tail == a.slots;
+  const int64_t out_row = (int64_t)(tok0 + my_tok) * q_heads + my_head;
+  const int64_t part_row = all_cut ? (int64_t)split * a.n * q_heads + out_row : (((int64_t)from_end * a.heads + kvh) * a.splits + split) * kRows + row;
   if (split >= parts) {                  // nothing: a weight of zero
-    if (live && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(-INFINITY, 0.f);
+    if (all_cut && live && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(-INFINITY, 0.f);
     return;
   }
   const int32_t* table = a.paged.table + (int64_t)b * a.paged.max_blocks;
@@ -452,7 +481,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   sum = with_partner(sum, [](float x, float y) { return x + y; });
   if (!live) return;
   if (parts == 1) {
-    if (a.splits > 1 && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(0.f, kWhole);
+    if (all_cut && a.splits > 1 && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(0.f, kWhole);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -485,20 +514,15 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     }
 }
 
-// The splits of a row put together, in the order of their numbers: a wave takes a row, a lane D / 64 channels (D = 32: half of the
-// lanes one each).
+// The parts of a row put together, in the order of their numbers, by a wave: a lane takes D / 64 channels (D = 32: half of the lanes one
+// each).  row: the first part's, the others `step` rows apart; to: the row of the output.
 template <int D>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ ml_part, int splits, int64_t n_rows, int q_heads,
-                                                          const int32_t* __restrict__ starts, int n_b, int n, void* __restrict__ o, int o_dtype) {
+__device__ __forceinline__ void merge_row(const float* __restrict__ o_part, const float* __restrict__ ml_part, int parts, int64_t row, int64_t step, int64_t to,
+                                          int lane, void* __restrict__ o, int o_dtype) {
   constexpr int E = D == 128 ? 2 : 1;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= n_rows) return;
-  const int tok = (int)(row / q_heads);
-  if (tok < starts[0] || tok >= min(starts[n_b], n)) return;
   float m = -INFINITY, l = 0.f;
-  if (lane < splits) {
-    const float2 v = *reinterpret_cast<const float2*>(&ml_part[2 * (lane * n_rows + row)]);
+  if (lane < parts) {
+    const float2 v = *reinterpret_cast<const float2*>(&ml_part[2 * (row + lane * step)]);
     m = v.x;
     l = v.y;
   }
@@ -507,10 +531,10 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
   const float w = m == -INFINITY ? 0.f : exp2f(m - top);
   const float den = across_lanes<0x3f>(w * l, [](float x, float y) { return x + y; });
   float x[E] = {};
-  for (int s = 0; s < splits; ++s) {
+  for (int s = 0; s < parts; ++s) {
     const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
     if (f == 0.f) continue;
-    const float* p = &o_part[(s * n_rows + row) * D + E * (lane & (D / E - 1))];
+    const float* p = &o_part[(row + s * step) * D + E * (lane & (D / E - 1))];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = fmaf(p[e], f, x[e]);
   }
@@ -518,8 +542,37 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float r = over_sum(x[e], den);
-    if (o_dtype == CKV_BF16) reinterpret_cast<uint16_t*>(o)[row * D + E * lane + e] = f32_to_bf16_rne(r);
-    else reinterpret_cast<float*>(o)[row * D + E * lane + e] = r;
+    if (o_dtype == CKV_BF16) reinterpret_cast<uint16_t*>(o)[to * D + E * lane + e] = f32_to_bf16_rne(r);
+    else reinterpret_cast<float*>(o)[to * D + E * lane + e] = r;
+  }
+}
+
+// All rows, a wave each.
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a, int64_t n_rows) {
+  const int lane = threadIdx.x & 63, q_heads = a.heads << a.g_shift;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= n_rows) return;
+  const int tok = (int)(row / q_heads);
+  if (tok < a.starts[0] || tok >= min(a.starts[a.n_b], a.n)) return;
+  merge_row<D>(a.o_part, a.ml_part, a.splits, row, n_rows, row, lane, a.o, a.o_dtype);
+}
+
+// The rows of the places that were cut: a workgroup takes kMergeRows of a place and a KV head.
+constexpr int kMergeRows = 16;
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge_tail_kernel(ChunkArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t_shift = __builtin_ctz(kRows) - a.g_shift;
+  const int group = blockIdx.x / (kRows / kMergeRows), row0 = blockIdx.x % (kRows / kMergeRows) * kMergeRows, kvh = group % a.heads;
+  const int from_end = group / a.heads;
+  int slot = from_end, used, b, part;
+  Rows w;
+  if (!in_order(a, t_shift, lane, true, slot, used, b, part) || !rows_of(a, t_shift, b, part, w)) return;
+  const int parts = parts_of(a, w.seen);
+  if (parts == 1) return;
+  for (int r = row0 + wave; r < min(row0 + kMergeRows, w.tokens << a.g_shift); r += 4) {
+    const int64_t to = (((int64_t)(w.tok0 + (r >> a.g_shift)) * a.heads + kvh) << a.g_shift) + (r & ((1 << a.g_shift) - 1));
+    merge_row<D>(a.o_part, a.ml_part, parts, ((int64_t)group * a.splits) * kRows + r, kRows, to, lane, a.o, a.o_dtype);
   }
 }
 
@@ -527,42 +580,58 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const float* __restric
 
 namespace {
 constexpr int kMostSplits = 64, kLeastSpan = 128, kSpan = 4096, kRounds = 3;
+constexpr int kTailSplits = 4, kTailSpan = 512, kTailEighths = 4;
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+int64_t most(int64_t a, int64_t b) { return a > b ? a : b; }
 // the most parts that a call of up to max_len tokens is cut into
 int64_t most_splits(int max_len) { return least(up(max_len, kLeastSpan), kMostSplits); }
 int groups_at_once() { return 2 * cu_count(); }
+int64_t tail_places(int heads) { return up(groups_at_once() * (int64_t)kTailEighths / 8, heads); }
 }  // namespace
 
-// How the tokens are cut: so that every place on the chip has work, down to spans of kLeastSpan tokens; and down to kSpan tokens into
-// kRounds times as many workgroups as there are places, so that those that finish last are few.
+// How the tokens are cut.  Few places: so that every workgroup that fits on the chip has work, down to spans of kLeastSpan tokens; and down
+// to kSpan tokens into kRounds times as many workgroups as fit, so that those that finish last are few.
 // us with kRounds, kSpan = 3, 4096 / 3, 2048 / 6, 4096 / 10, 1024: 16 requests of 1 to 8 tokens over 32768 313 / 341 / 310 / 349; 39 single
 // tokens and 1999 of another over 16384 922 / 930 / 953 / 1008.  33 tokens over 515 with kLeastSpan 128 / 256 / 512: 15.4 / 16.5 / 19.3.
+// Places enough for kRounds rounds: the last half of a round (kTailEighths) in up to kTailSplits parts.  Four turns of 1024 to 2048 tokens over
+// 16384 are three rounds and a little: 1537 us with whole places, 1434 so, 1428 with 8 parts, 1440 with a quarter of a round, 1446 with
+// a whole one; a prompt of 16384 tokens stays at 2050.  From one round on (kRounds 1): 39 single tokens beside 1999 975, not 908,
+// 9 x 700 tokens over 1500 states 56, not 40.
 ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
   ChunkCut cut;
-  cut.slots = n / (kRows / (q_heads / heads)) + n_b;
+  cut.slots = n / (kRows / (q_heads / heads)) + (n_b <= 64 && n < n_b ? (int)most(n, 1) : n_b);
   const int64_t groups = (int64_t)cut.slots * heads;
+  if (groups >= (int64_t)kRounds * groups_at_once()) {
+    cut.span = (int)(up(most(up(max_len, kTailSplits), kTailSpan), 64) * 64);
+    cut.tail = n_b <= 64 && max_len > cut.span ? (int)least(tail_places(heads), cut.slots - 1) : 0;
+    cut.splits = cut.tail ? (int)up(max_len, cut.span) : 1;
+    return cut;
+  }
   const int64_t fill = least(up(groups_at_once(), groups), up(max_len, kLeastSpan));
   const int64_t even = least(up((int64_t)kRounds * groups_at_once(), groups), up(max_len, kSpan));
-  const int64_t splits = least(fill > even ? fill : even, kMostSplits);
+  const int64_t splits = least(most(fill, even), kMostSplits);
   cut.span = (int)(up(up(max_len, splits), 64) * 64);
   cut.splits = (int)up(max_len, cut.span);
+  cut.tail = cut.slots;
   return cut;
 }
 
 // (max, sum) pairs, up to the next 16 bytes, then the sums of values
-size_t chunk_workspace_bytes(int64_t rows, int splits, int dim) {
-  if (splits <= 1) return 0;
-  const size_t parts = (size_t)rows * splits;
-  return (parts * 8 + 15) / 16 * 16 + parts * dim * 4;
+static size_t part_bytes(int64_t parts, int dim) { return (size_t)(parts * 8 + 15) / 16 * 16 + (size_t)parts * dim * 4; }
+static int64_t part_rows(const ChunkCut& cut, int heads, int64_t rows) {
+  return cut.splits <= 1 ? 0 : cut.splits * (cut.tail == cut.slots ? rows : (int64_t)cut.tail * heads * kRows);
 }
 
-// Rows are cut where there are fewer than kRounds * groups_at_once() places for workgroups, of kRows rows at most, into as many parts
-// more as make up the difference; and none into more than most_splits().
-size_t chunk_reserve_bytes(int q_heads, int n, int max_len, int dim) {
-  const int64_t most = most_splits(max_len), full = (int64_t)kRows * kRounds * groups_at_once(), rows = (int64_t)n * q_heads;
-  const int64_t parts = least(rows * most, full + least(rows, full));
-  return most <= 1 ? 0 : (size_t)(parts * 8 + 15) / 16 * 16 + (size_t)parts * dim * 4;
+size_t chunk_workspace_bytes(const ChunkCut& cut, int heads, int64_t rows, int dim) { return part_bytes(part_rows(cut, heads, rows), dim); }
+
+// All places are cut where there are fewer than kRounds * groups_at_once() of them, of kRows rows at most, into as many parts more as make
+// up the difference; and none into more than most_splits().  A tail is cut where a batch of up to 64 can have as many places.
+size_t chunk_reserve_bytes(int heads, int q_heads, int n, int max_len, int dim) {
+  const int64_t some = most_splits(max_len), full = (int64_t)kRows * kRounds * groups_at_once(), rows = (int64_t)n * q_heads;
+  if (some <= 1) return 0;
+  const bool tail = ((int64_t)n / (kRows / (q_heads / heads)) + (n < 64 ? n : 64)) * heads >= (int64_t)kRounds * groups_at_once();
+  return part_bytes(most(least(rows * some, full + least(rows, full)), tail ? tail_places(heads) * heads * kRows * kTailSplits : 0), dim);
 }
 
 hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t st) {
@@ -575,12 +644,12 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
   a.paged = c.paged; a.lens = c.lens; a.max_len = c.max_len; a.heads = c.heads;
   a.g_shift = __builtin_ctz(c.q_heads / c.heads);
   a.c = c.scale * kLog2e;
-  a.causal = c.causal; a.slots = cut.slots; a.splits = cut.splits; a.span = cut.span;
+  a.causal = c.causal; a.slots = cut.slots; a.splits = cut.splits; a.span = cut.span; a.tail = cut.tail;
   a.o = c.o; a.o_dtype = c.o_dtype;
   const int64_t rows = (int64_t)c.n * c.q_heads;
   a.ml_part = static_cast<float*>(c.workspace);
-  a.o_part = a.ml_part + (rows * cut.splits * 2 + 3) / 4 * 4;
-  const dim3 grid((unsigned)((int64_t)cut.slots * c.heads * cut.splits));
+  a.o_part = a.ml_part + (part_rows(cut, c.heads, rows) * 2 + 3) / 4 * 4;
+  const dim3 grid((unsigned)((cut.slots + (int64_t)cut.tail * (cut.splits - 1)) * c.heads));
   hipError_t e = hipErrorInvalidValue;
 #define CKV_CHUNK_DEG(T, D, DEG)                                                                                             \
   do {                                                                                                                \
@@ -595,8 +664,10 @@ hipError_t launch_chunk_attn(const ChunkCall& c, int dtype, int dim, hipStream_t
     e = hipGetLastError();                                                                                            \
     if (e == hipSuccess && cut.splits > 1) {                                                                          \
       ScopedTimer t("chunk_merge", st);                                                                               \
-      hipLaunchKernelGGL((chunk_merge_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a.o_part, a.ml_part, \
-                         cut.splits, rows, c.q_heads, c.starts, c.n_b, c.n, c.o, c.o_dtype);                          \
+      if (cut.tail == cut.slots)                                                                                      \
+        hipLaunchKernelGGL((chunk_merge_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a, rows);     \
+      else                                                                                                            \
+        hipLaunchKernelGGL((chunk_merge_tail_kernel<D>), dim3((unsigned)(cut.tail * c.heads * (kRows / kMergeRows))), dim3(256), 0, st, a); \
       e = hipGetLastError();                                                                                          \
     }                                                                                                                 \
   } while (0)

@@ -105,6 +105,18 @@ def test_against_the_oracle(dtype, heads, group, dim, block, lens, new, degrees,
         assert torch.equal(again[:starts[-1]], out[:starts[-1]])
 
 
+@pytest.mark.parametrize("dtype,heads,group,dim,block,batch,most,new,degrees,causal", [
+    ("bf16", 14, 8, 64, 16, 4, 1100, (450, 450), True, True), ("bf16", 32, 4, 128, 16, 60, 1200, (1, 1), False, True),
+    ("f32", 32, 2, 64, 8, 50, 1300, (1, 3), True, True), ("bf16", 40, 1, 64, 32, 64, 700, (0, 2), False, False),
+    ("bf16", 32, 4, 64, 16, 65, 900, (0, 3), True, True), ("bf16", 16, 2, 128, 16, 64, 511, (1, 90), True, True)])
+def test_more_rows_than_the_chip_has_places(dtype, heads, group, dim, block, batch, most, new, degrees, causal):
+    """Where the rows fill the chip several times over only the last of them are cut, or none."""
+    rng = np.random.default_rng(batch)
+    fresh = [int(x) for x in rng.integers(new[0], new[1] + 1, batch)]
+    lens = [max(int(x), y) for x, y in zip(rng.integers(most // 2, most + 1, batch), fresh)]
+    test_against_the_oracle(dtype, heads, group, dim, block, lens, fresh, degrees, causal)
+
+
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 def test_tokens_that_are_not_seen_do_not_reach_a_row(dtype, dim):
     """Infinities and NaN in keys and values behind a row, in tokens of degree 0, in the rest of a page and under entries outside the pool."""
