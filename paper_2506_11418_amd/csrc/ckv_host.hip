@@ -1204,7 +1204,7 @@ int ckv_paged_copy(const int32_t* moves, int32_t n_moves, void* K_pool, void* V_
   const int e = ckv::elem_bytes(pl->dtype);
   const int64_t page = (int64_t)pl->heads * pl->block_size * pl->dim * e;
   if (n_moves < 0 || n_moves > kMostEntries || (int64_t)pl->heads * pl->dim * e > INT32_MAX / 1024) return CKV_ESHAPE;
-  if ((page / 16384 + 1) * n_moves > kMostGroups) return CKV_EUNSUPPORTED;
+  if (2 * (page / 16384 + 1) * n_moves > kMostGroups) return CKV_EUNSUPPORTED;
   if (n_moves == 0) return CKV_OK;
   if (!moves || !K_pool || !V_pool || !bounds != !mass) return CKV_EINVAL;
   if (((uintptr_t)K_pool | (uintptr_t)V_pool | (uintptr_t)bounds) % 16 || misaligned4({moves, deg_pool, mass})) return CKV_EALIGN;

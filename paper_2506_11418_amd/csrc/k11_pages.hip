@@ -407,17 +407,20 @@ __global__ __launch_bounds__(kScanThreads) void compact_small_kernel(int32_t* __
 }
 
 // ---- copy ----------------------------------------------------------------------------------------
-// Pages by pairs (from, to).  A workgroup takes kPieces 16-byte pieces of the keys and of the values: of several pages where they are
-// small (`group` of them), else part of one.
-// Loads go through the caches and stores past them: a prompt that several rows continue is read from memory once (1024 blocks to 7 rows and
-// 33 x 65 of 64 KB to 2, with the trims: 190 and 99 us, against 229 and 147 past both), where every block moves once it costs little
-// (64 x 8192 tokens: 682 us against 643); stores through them 261 and 163.  Two pieces a thread: four 188 and 108, one 208 and 104.
-constexpr int kPerThread = 2, kPieces = kThreads * kPerThread;
+// Pages by pairs (from, to).  A workgroup takes kPieces 16-byte pieces of the keys, in the grid's second half of the values: of several
+// pages where they are small (`group` of them), else part of one.  Loads go through the caches and stores past them: what several
+// rows continue is read from memory once.  us for 7 copies of 1024 blocks of 64 KB / 2 of each of 33 x 65 of 128 KB / 2 x 16384 blocks moved,
+// with what frees and deals them: 168 / 107 / 642; loads past the caches as well 229 / 147 / 643; stores through them 261 / 163;
+// keys and values of a page by one workgroup 186 / 98 / 666; eight pieces a thread 165 / 113 / 675, two 169 / 106 / 652.
+constexpr int kPerThread = 4, kPieces = kThreads * kPerThread;
 __global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __restrict__ moves, int n_moves, unsigned char* __restrict__ K,
                                                               unsigned char* __restrict__ V, int32_t* __restrict__ deg, unsigned char* __restrict__ bounds,
                                                               int32_t* __restrict__ mass, int n_blocks, int page_pieces, int rows, int heads,
                                                               int bound_pieces, int group, int parts) {
-  const int m0 = blockIdx.x / parts * group, part = blockIdx.x % parts, tid = threadIdx.x;
+  const bool values = blockIdx.x >= gridDim.x / 2;
+  const int id = values ? blockIdx.x - gridDim.x / 2 : blockIdx.x;
+  unsigned char* pool = values ? V : K;
+  const int m0 = id / parts * group, part = id % parts, tid = threadIdx.x;
   const int n = min(group, n_moves - m0);
   auto pair = [&](int m, int& from, int& to) {
     from = moves[2 * m];
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __r
     return (unsigned)from < (unsigned)n_blocks && (unsigned)to < (unsigned)n_blocks && from != to;
   };
   const int p0 = part * kPieces, total = parts > 1 ? min(kPieces, page_pieces - p0) : n * page_pieces;
-  uint4 k[kPerThread], v[kPerThread];
+  uint4 piece[kPerThread];
   int64_t at[kPerThread];
 #pragma unroll
   for (int i = 0; i < kPerThread; ++i) {
@@ -437,18 +440,14 @@ __global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __r
       if (pair(m0 + m, from, to)) {
         at[i] = ((int64_t)to * page_pieces + p) * 16;
         const int64_t src = ((int64_t)from * page_pieces + p) * 16;
-        k[i] = *reinterpret_cast<const uint4*>(K + src);
-        v[i] = *reinterpret_cast<const uint4*>(V + src);
+        piece[i] = *reinterpret_cast<const uint4*>(pool + src);
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < kPerThread; ++i)
-    if (at[i] >= 0) {
-      stg16_stream(K + at[i], k[i]);
-      stg16_stream(V + at[i], v[i]);
-    }
-  if (part) return;
+    if (at[i] >= 0) stg16_stream(pool + at[i], piece[i]);
+  if (values || part) return;
   for (int m = 0; m < n; ++m) {
     int from, to;
     if (!pair(m0 + m, from, to)) continue;
@@ -528,7 +527,7 @@ hipError_t launch_paged_copy(const int32_t* moves, int n_moves, void* K, void* V
   ScopedTimer t("paged_copy", st);
   const int pieces = heads * block_size * (row_bytes / 16);
   const int group = pieces < kPieces ? kPieces / pieces : 1, parts = div_up(pieces, kPieces);
-  hipLaunchKernelGGL(paged_copy_kernel, dim3((unsigned)(div_up(n_moves, group) * parts)), dim3(kThreads), 0, st, moves, n_moves,
+  hipLaunchKernelGGL(paged_copy_kernel, dim3(2u * (unsigned)(div_up(n_moves, group) * parts)), dim3(kThreads), 0, st, moves, n_moves,
                      static_cast<unsigned char*>(K), static_cast<unsigned char*>(V), deg, static_cast<unsigned char*>(bounds), mass, n_blocks, pieces,
                      heads * block_size, heads, heads * 2 * (row_bytes / 16), group, parts);
   return hipGetLastError();
