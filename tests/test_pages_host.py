@@ -38,7 +38,9 @@ def _chunk(**kw):
     (dict(bytes=0), -4), (dict(bytes=1000), -4), (dict(scale=1e-31), -5), (dict(scale=2e30), -5), (dict(scale=float("inf")), -5),
     (dict(o=_p(1, 4096)), -1), (dict(o=_p(3, POOL - 16)), -1), (dict(o=_p(4)), -1), (dict(o=_p(5)), -1), (dict(o=_p(6, 16)), -1), (dict(o=_p(9)), -1),
     (dict(ws=_p(1)), -1), (dict(ws=_p(3, 64)), -1), (dict(ws=_p(7)), -1), (dict(ws=_p(2)), -1), (dict(lens=_p(8, 32)), -1), (dict(starts=_p(8)), -1),
-    (dict(pl=_pl(batch=65536)), -5),
+    (dict(pl=_pl(batch=65536)), -5), (dict(pl=_pl(batch=1, bs=1, width=(1 << 31) - 1000), max_len=(1 << 31) - 1), -5),
+    (dict(pl=_pl(batch=1, bs=1, width=(1 << 31) - 1000), max_len=(1 << 31) - 1024), -5), (dict(n=(1 << 30) + 1), -5), (dict(n=1 << 30), -5),
+    (dict(scale=float("-inf"), q=Z), -1), (dict(scale=1e-30, o=_p(1)), -1), (dict(scale=1e30, o=_p(1)), -1),
 ])
 def test_chunk_attention_refuses(kw, status):
     assert _chunk(**kw) == status
@@ -145,7 +147,8 @@ def test_compact_workspace():
 
 @pytest.mark.parametrize("kw,status", [
     (dict(moves=Z), -1), (dict(K=Z), -1), (dict(V=Z), -1), (dict(bounds=Z), -1), (dict(mass=Z), -1), (dict(n=-1), -2), (dict(n=(1 << 30) + 1), -2),
-    (dict(n=1 << 30), -5), (dict(pl=_pl(dim=100)), -3), (dict(pl=_pl(bs=12)), -2), (dict(pl=_pl(heads=1 << 14, dim=1 << 8)), -2),
+    (dict(n=1 << 30), -5), (dict(n=2796202, moves=_p(3, 64)), -1), (dict(n=2796203, moves=_p(3, 64)), -5),
+    (dict(pl=_pl(dim=100)), -3), (dict(pl=_pl(bs=12)), -2), (dict(pl=_pl(heads=1 << 14, dim=1 << 8)), -2),
     (dict(K=_p(2, 8)), -3), (dict(bounds=_p(5, 4)), -3), (dict(moves=_p(1, 2)), -3), (dict(mass=_p(6, 1)), -3),
     (dict(V=_p(2, POOL - 16)), -1), (dict(moves=_p(3, 64)), -1), (dict(deg=_p(2)), -1), (dict(bounds=_p(4, 16)), -1), (dict(mass=_p(1, 8)), -1),
 ])
