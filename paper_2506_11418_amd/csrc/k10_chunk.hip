@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256) void chunk_merge_tail_kernel(ChunkArgs a) {
 
 namespace {
 constexpr int kMostSplits = 64, kLeastSpan = 128, kSpan = 4096, kRounds = 3;
-constexpr int kTailSplits = 4, kTailSpan = 512, kTailEighths = 4;
+constexpr int kTailSplits = 4, kTailEighths = 4;
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t most(int64_t a, int64_t b) { return a > b ? a : b; }
@@ -605,7 +605,8 @@ int64_t tail_places(int heads) { return up(groups_at_once() * (int64_t)kTailEigh
 // to kSpan tokens into kRounds times as many workgroups as fit, so that those that finish last are few.
 // us with kRounds, kSpan = 3, 4096 / 3, 2048 / 6, 4096 / 10, 1024: 16 requests of 1 to 8 tokens over 32768 313 / 341 / 310 / 349; 39 single
 // tokens and 1999 of another over 16384 922 / 930 / 953 / 1008.  33 tokens over 515 with kLeastSpan 128 / 256 / 512: 15.4 / 16.5 / 19.3.
-// Places enough for kRounds rounds: the last half of a round (kTailEighths) in up to kTailSplits parts.  Four turns of 1024 to 2048 tokens over
+// Places enough for kRounds rounds: the last half of a round (kTailEighths) in up to kTailSplits parts, of kSpan tokens or more (of 512 or more,
+// 64 turns of 100 over 1000 took 176 us, not 154, and 8 of 1000 over 2000 274, not 252).  Four turns of 1024 to 2048 tokens over
 // 16384 are three rounds and a little: 1537 us with whole places, 1434 so, 1428 with 8 parts, 1440 with a quarter of a round, 1446 with
 // a whole one; a prompt of 16384 tokens stays at 2050.  From one round on (kRounds 1): 39 single tokens beside 1999 975, not 908,
 // 9 x 700 tokens over 1500 states 56, not 40.
@@ -614,7 +615,7 @@ ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
   cut.slots = n / (kRows / (q_heads / heads)) + (n_b <= 64 && n < n_b ? (int)most(n, 1) : n_b);
   const int64_t groups = (int64_t)cut.slots * heads;
   if (groups >= (int64_t)kRounds * groups_at_once()) {
-    cut.span = (int)(up(most(up(max_len, kTailSplits), kTailSpan), 64) * 64);
+    cut.span = (int)(up(most(up(max_len, kTailSplits), kSpan), 64) * 64);
     cut.tail = n_b <= 64 && max_len > cut.span ? (int)least(tail_places(heads), cut.slots - 1) : 0;
     cut.splits = cut.tail ? (int)up(max_len, cut.span) : 1;
     return cut;

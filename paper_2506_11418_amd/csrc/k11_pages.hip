@@ -413,8 +413,9 @@ __global__ __launch_bounds__(kScanThreads) void compact_small_kernel(int32_t* __
 // Pages by pairs (from, to).  A workgroup takes kPieces 16-byte pieces of the keys, in the grid's second half of the values: of several
 // pages where they are small (`group` of them), else part of one.  Loads go through the caches and stores past them: what several
 // rows continue is read from memory once.  us for 7 copies of 1024 blocks of 64 KB / 2 of each of 33 x 65 of 128 KB / 2 x 16384 blocks moved,
-// with what frees and deals them: 168 / 107 / 642; loads past the caches as well 229 / 147 / 643; stores through them 261 / 163;
-// keys and values of a page by one workgroup 186 / 98 / 666; eight pieces a thread 165 / 113 / 675, two 169 / 106 / 652.
+// with what deals and frees them, on pages that no cache holds: 166 / 134 / 643; loads past the caches as well 217 / 140 / 627; keys and values
+// of a page by one workgroup 188 / 137 / 666.  Repeated on the same pages: 168 / 107 / 642; stores through the caches 261 / 163; eight pieces a
+// thread 165 / 113 / 675, two 169 / 106 / 652.
 constexpr int kPerThread = 4, kPieces = kThreads * kPerThread;
 __global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __restrict__ moves, int n_moves, unsigned char* __restrict__ K,
                                                               unsigned char* __restrict__ V, int32_t* __restrict__ deg, unsigned char* __restrict__ bounds,

@@ -117,6 +117,36 @@ def test_more_rows_than_the_chip_has_places(dtype, heads, group, dim, block, bat
     test_against_the_oracle(dtype, heads, group, dim, block, lens, fresh, degrees, causal)
 
 
+@pytest.mark.parametrize("dtype,dim,causal,o_dtype", [("bf16", 64, True, torch.bfloat16), ("bf16", 128, False, torch.float32), ("f32", 32, True, torch.float32)])
+def test_the_last_rows_of_many_are_cut(dtype, dim, causal, o_dtype):
+    """Long turns that fill the chip several times over, with some rows out of each stretch of 64 tokens against the oracle."""
+    lens, new, heads, G = [9700, 9001, 9200], [4200, 4203, 4201], 2, 8
+    print(f"last rows {dtype} {dim} {causal}", flush=True)
+    c = Cache(83, lens, heads, dim, 16, dtype, True)
+    K, V, deg, table, n = c.gpu()
+    starts = _starts(new, lead=2)
+    q = _queries(15, starts[-1], heads * G, dim, c.dtype)
+    ws = torch.full((ckv.paged_chunk_attn_workspace(ckv.paged_layout_of(K, table), heads * G, q.shape[0], 9700),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full(q.shape, 7.0, dtype=o_dtype, device=DEV)
+    ckv.paged_chunk_attn(q.to(DEV), K, V, deg, table, n, _dev(starts), 9700, causal=causal, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    assert (out[:2] == 7.0).all()
+    rng, scale = np.random.default_rng(2), _scale(dim)
+    for b in range(3):
+        rows = np.array([min(t + int(rng.integers(0, 64)), new[b] - 1) for t in range(0, new[b], 64)])
+        ids, h = table[b, :-(-lens[b] // 16)].cpu().long(), int(rng.integers(0, heads))
+        k, v, d = (p[ids, h].reshape(-1, p.shape[-1])[:lens[b]] for p in (c.K, c.V, c.deg[..., None]))
+        at, cols = torch.from_numpy(starts[b] + rows), slice(h * G, (h + 1) * G)
+        seen = lens[b] - new[b] + rows + 1 if causal else np.full(len(rows), lens[b])
+        o, a, x = po.chunk_attention(f64(q[at, cols]), f64(k), f64(v), i64(d[:, 0]), seen, scale)
+        e = (dim + 8) * 2.0**-24 * (x * scale + math.log(9)) + 2.0**-22
+        u = 2 * U[c.dtype] if c.dtype == torch.bfloat16 else 0.0
+        _close(out[at.to(DEV), cols], o, (u + 2 * e[..., None] + (lens[b] + 128) * 2.0**-24) * a, o_dtype, f"sequence {b}")
+    again = torch.zeros_like(out)
+    ckv.paged_chunk_attn(q.to(DEV), K, V, deg, table, n, _dev(starts), 9700, causal=causal, out=again, workspace=ws)
+    assert torch.equal(again[2:], out[2:])
+
+
 @pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 def test_tokens_that_are_not_seen_do_not_reach_a_row(dtype, dim):
     """Infinities and NaN in keys and values behind a row, in tokens of degree 0, in the rest of a page and under entries outside the pool."""
