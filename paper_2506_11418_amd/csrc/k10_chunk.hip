@@ -57,38 +57,49 @@ struct Rows {
   int b, tok0, tokens, len, pos0, seen;  // pos0: position of the first of these tokens; seen: tokens that any of them sees
 };
 
-// Which rows the workgroup at `slot` has, of a batch of up to 64: the longest sequence's first, so that those that start last are the shortest,
-// and of a sequence the last ones, which see most.  A lane holds a sequence.  used: places that have rows.
-// back: count from the end of those (`slot` becomes the place).  All lanes of the wave take part.
-__device__ __forceinline__ bool in_order(const ChunkArgs& a, int t_shift, int lane, bool back, int& slot, int& used, int& b, int& part) {
-  const int at = min(lane, a.n_b - 1), first = min(max(a.starts[at], 0), a.n), last = min(max(a.starts[at + 1], 0), a.n);
-  const int count = lane < a.n_b ? (max(last - first, 0) + (1 << t_shift) - 1) >> t_shift : 0, len = a.lens[at];
-  int before = 0;
-  used = 0;
-  for (int i = 0; i < a.n_b; ++i) {
-    const int l = __builtin_amdgcn_readlane(len, i), c = __builtin_amdgcn_readlane(count, i);
-    if (l > len || (l == len && i < lane)) before += c;
-    used += c;
-  }
-  if (back) slot = used - 1 - slot;
-  const uint64_t mine = __ballot(slot >= before && slot < before + count);
-  if (!mine) return false;
-  b = (int)__builtin_ctzll(mine);
-  part = __builtin_amdgcn_readlane(before + count, b) - 1 - slot;
-  return true;
-}
-
-__device__ __forceinline__ bool rows_of(const ChunkArgs& a, int t_shift, int b, int part, Rows& r) {
-  const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
+__device__ __forceinline__ bool rows_of(const ChunkArgs& a, int t_shift, int b, int part, int first, int last, int len, Rows& r) {
   r.b = b;
   r.tok0 = first + (part << t_shift);
   r.tokens = min(last - r.tok0, 1 << t_shift);
   if (part < 0 || r.tokens <= 0) return false;
   const int64_t cap = (int64_t)a.paged.max_blocks << a.paged.shift;
-  r.len = (int)min((int64_t)min(max(a.lens[b], 0), a.max_len), cap);
+  r.len = (int)min((int64_t)min(max(len, 0), a.max_len), cap);
   r.pos0 = r.len - (last - r.tok0);
   r.seen = a.causal ? max(min(r.pos0 + r.tokens, r.len), 0) : r.len;
   return true;
+}
+
+// What a workgroup's waves tell each other of an order.
+struct Order { int before[kWaves][64], used[kWaves]; };
+
+// Which rows the workgroup at `slot` has, of a batch of up to 64: the longest sequence's first, so that those that start last are the shortest,
+// and of a sequence the last ones, which see most.  A lane holds a sequence and counts the places before its own, a quarter of the
+// sequences in each wave (all of them in every wave: 4.5 us more a workgroup beside another, with 64 sequences).  used: places that have rows.
+// back: count from the end of those (`slot` becomes the place).  All threads of the workgroup take part.
+__device__ __forceinline__ bool in_order(const ChunkArgs& a, int t_shift, int wave, int lane, bool back, Order& s, int& slot, int& used, Rows& r) {
+  const int at = min(lane, a.n_b - 1), first = min(max(a.starts[at], 0), a.n), last = min(max(a.starts[at + 1], 0), a.n);
+  const int count = lane < a.n_b ? (max(last - first, 0) + (1 << t_shift) - 1) >> t_shift : 0, len = a.lens[at];
+  int before = 0;
+  used = 0;
+  for (int i = wave * (64 / kWaves); i < min((wave + 1) * (64 / kWaves), a.n_b); ++i) {
+    const int l = __builtin_amdgcn_readlane(len, i), c = __builtin_amdgcn_readlane(count, i);
+    if (l > len || (l == len && i < lane)) before += c;
+    used += c;
+  }
+  s.before[wave][lane] = before;
+  if (lane == 0) s.used[wave] = used;
+  __syncthreads();
+  before = used = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += s.before[w][lane];
+    used += __builtin_amdgcn_readfirstlane(s.used[w]);
+  }
+  if (back) slot = used - 1 - slot;
+  const uint64_t mine = __ballot(slot >= before && slot < before + count);
+  if (!mine) return false;
+  const int b = (int)__builtin_ctzll(mine), part = __builtin_amdgcn_readlane(before + count, b) - 1 - slot;
+  return rows_of(a, t_shift, b, part, __builtin_amdgcn_readlane(first, b), __builtin_amdgcn_readlane(last, b), __builtin_amdgcn_readlane(len, b), r);
 }
 
 // These rows' tokens are cut into as many equal parts as spans of a.span tokens hold them.
@@ -149,15 +160,17 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ __attribute__((aligned(16))) typename std::conditional<L::BF16, uint4, float>::type s_bias[2][DEG ? L::TILE : 1];
   __shared__ uint64_t s_valid[2], s_odd;                 // a tile's tokens that count; those with a value that is no finite number
   __shared__ int s_seq;
+  __shared__ Order s_order;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
 
   // ---- which rows, which tokens: first every place's first part, then the others of the places that are cut
   const int kvh = blockIdx.x % a.heads, place = blockIdx.x / a.heads;
   const int t_shift = __builtin_ctz(kRows) - a.g_shift;  // tokens of a workgroup
   const int split = place < a.slots ? 0 : 1 + (place - a.slots) / a.tail;
-  int b, part, used = a.slots, slot = split ? a.tail - 1 - (place - a.slots) % a.tail : place;
+  int used = a.slots, slot = split ? a.tail - 1 - (place - a.slots) % a.tail : place;
+  Rows mine;
   if (a.n_b <= 64) {
-    if (!in_order(a, t_shift, lane, split > 0, slot, used, b, part)) return;
+    if (!in_order(a, t_shift, wave, lane, split > 0, s_order, slot, used, mine)) return;
   } else {
     // Sequence b has the places from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
     if (split) slot = a.slots - 1 - slot;
@@ -167,13 +180,12 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
     for (int i = tid; i < a.n_b; i += kThreads) before += (min(max(a.starts[i], 0), a.n) >> t_shift) + i <= slot;
     if (before) atomicAdd(&s_seq, before);
     __syncthreads();
-    b = s_seq - 1;
+    const int b = s_seq - 1;
     if (b < 0) return;
-    part = slot - (min(max(a.starts[b], 0), a.n) >> t_shift) - b;
+    const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
+    if (!rows_of(a, t_shift, b, slot - (first >> t_shift) - b, first, last, a.lens[b], mine)) return;
   }
-  Rows mine;
-  if (!rows_of(a, t_shift, b, part, mine)) return;
-  const int tok0 = mine.tok0, tokens = mine.tokens, len = mine.len, pos0 = mine.pos0, seen = mine.seen;
+  const int b = mine.b, tok0 = mine.tok0, tokens = mine.tokens, len = mine.len, pos0 = mine.pos0, seen = mine.seen;
   const int rows = tokens << a.g_shift;
   const int row = wave * 32 + col;
   const bool live = row < rows;
@@ -576,9 +588,10 @@ __global__ __launch_bounds__(256) void chunk_merge_tail_kernel(ChunkArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t_shift = __builtin_ctz(kRows) - a.g_shift;
   const int group = blockIdx.x / (kRows / kMergeRows), row0 = blockIdx.x % (kRows / kMergeRows) * kMergeRows, kvh = group % a.heads;
   const int from_end = group / a.heads;
-  int slot = from_end, used, b, part;
+  __shared__ Order s_order;
+  int slot = from_end, used;
   Rows w;
-  if (!in_order(a, t_shift, lane, true, slot, used, b, part) || !rows_of(a, t_shift, b, part, w)) return;
+  if (!in_order(a, t_shift, wave, lane, true, s_order, slot, used, w)) return;
   const int parts = parts_of(a, w.seen);
   if (parts == 1) return;
   for (int r = row0 + wave; r < min(row0 + kMergeRows, w.tokens << a.g_shift); r += 4) {
