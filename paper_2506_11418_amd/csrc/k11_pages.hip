@@ -77,9 +77,10 @@ __global__ __launch_bounds__(kThreads) void fork_count_kernel(const int32_t* __r
   if (tid == 0) need[b] = len < 0 ? -1 : s_count[0] + s_count[1] + s_count[2] + s_count[3];
 }
 
-// A launch of its own counts above this many entries: with it 64 entries take 10.1 us, 1024 10.7, 2048 10.5 and 8192 11.5, without it 8.7,
-// 10.4, 11.3 and 21.2 (replayed by a graph, with the two copies that restore the arguments).
-constexpr int kCountedEntries = 1024;
+// Up to kRowsHere rows of kEntriesHere entries together are counted by the workgroups that deal, two rows a wave; else a launch of its own
+// counts.  Replayed by a graph, with the two copies that restore the arguments, us here / by a launch: 2 rows of 32 8.7 / 10.1, 8 of 128
+// 10.0 / 10.8, 16 of 64 10.9 / 10.6, 64 of 128 21.2 / 11.5; 155 of 3, by themselves, 31 / 11.
+constexpr int kRowsHere = 8, kEntriesHere = 1024;
 // Every workgroup sums the rows' needs for itself and deals to its share of the rows; the last one to arrive writes what the others
 // have read: lengths, grants (which held the needs) and the number of free blocks.
 // dynamic LDS: 8 bytes a row
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void fork_deal_kernel(int32_t* __restrict
   int32_t* marks = free_list + kListHead + n_blocks;
   if (counted) {
     for (int b = tid; b < n_b; b += kThreads) s_need[b] = granted[b];
-  } else {                                 // few entries: each workgroup counts them all, a row a wave
+  } else {                                 // each workgroup counts them all, a row a wave
     for (int b = tid >> 6; b < n_b; b += kWaves) {
       const int len = continued(lens, source, b, n_b, max_blocks, shift);
       int count = len;
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(kThreads) void paged_copy_kernel(const int32_t* __r
 
 hipError_t launch_paged_fork(int32_t* table, int32_t* lens, const int32_t* source, int32_t* free_list, int n_b, int max_blocks, int n_blocks,
                              int shift, int32_t* moves, int n_moves, int32_t* granted, hipStream_t st) {
-  const bool counted = (int64_t)n_b * max_blocks > kCountedEntries;
+  const bool counted = n_b > kRowsHere || n_b * max_blocks > kEntriesHere;
   if (counted) {
     ScopedTimer t("fork_count", st);
     hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)n_b), dim3(kThreads), 0, st, table, lens, source, n_b, max_blocks, n_blocks, shift, granted);
