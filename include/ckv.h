@@ -413,7 +413,8 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
  *   workspace: scratch, whatever it holds (NULL where the size is 0); the size for an n and a max_len serves every smaller
  *            one and every batch.  Calls that share one must not overlap in time.
  * bf16: products on bf16 matrix instructions with fp32 sums, softmax weights rounded to bf16 (by 2^-8 at most) for the product with
- * the values; the result does not depend on anything but the arguments (no atomics on numbers).  fp32: fp32 throughout.
+ * the values; the result depends on nothing but the arguments and the number of CUs (no atomics on numbers).  fp32: fp32 throughout.
+ * Infinite values that a token sees leave it an infinity or NaN.
  * Supported: q_heads / heads in {1,2,4,8}; bf16 dim 64/128; fp32 dim 32/64/128; pools of fewer than 2^31 token rows;
  * n <= 2^30; sequences (max_len, or what the table holds) of up to 2^31 - 1025 tokens. */
 int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, size_t* bytes);
@@ -453,7 +454,8 @@ int ckv_paged_compact(int32_t* block_table, const int32_t* lens, int32_t* free_l
 /* Pages moves[i][0] into pages moves[i][1]: keys, values, degrees (deg_pool may be NULL), bounds and mass (of ckv_paged_bounds;
  * both or neither).  Pairs with a block outside the pool and pairs of equal blocks are passed over.  A block that is written
  * must be named once; one that is written and also read by another pair leaves, piece by piece, either
- * content there.  Of the layout batch and max_blocks are not looked at (they have to be positive).  A page's row of all heads is smaller than 2 MB. */
+ * content there.  Of the layout batch and max_blocks are not looked at (they have to be positive).  A page's row of all heads is smaller than 2 MB;
+ * n_moves 0..2^30, CKV_EUNSUPPORTED where 2 n_moves (16 KiB pieces of a page's keys + 1) reaches 2^24. */
 int ckv_paged_copy(const int32_t* moves, int32_t n_moves, void* K_pool, void* V_pool, int32_t* deg_pool, void* bounds, int32_t* mass,
                    const ckv_paged_layout* pl, void* hip_stream);
 
