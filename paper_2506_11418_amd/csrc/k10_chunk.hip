@@ -30,6 +30,7 @@ namespace {
 constexpr int kRows = 128;               // query rows of a workgroup
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr float kWhole = -1.f;           // in the place of a first part's sum: the row's output has been written
+constexpr float kNoPart = -2.f;          // in the place of a part's sum: there is no such part of this row, nothing else of it has been written
 constexpr float kSlack = 8.f;            // how far (log2) a logit may exceed the reference before the sums are rescaled
 
 constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100;   // kinds of instructions, for the order that the compiler is asked for
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   const int64_t out_row = (int64_t)(tok0 + my_tok) * q_heads + my_head;
   const int64_t part_row = all_cut ? (int64_t)split * a.n * q_heads + out_row : (((int64_t)from_end * a.heads + kvh) * a.splits + split) * kRows + row;
   if (split >= parts) {                  // nothing: a weight of zero
-    if (all_cut && live && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(-INFINITY, 0.f);
+    if (all_cut && live && half == 0) *reinterpret_cast<float2*>(&a.ml_part[2 * part_row]) = make_float2(-INFINITY, kNoPart);
     return;
   }
   const int32_t* table = a.paged.table + (int64_t)b * a.paged.max_blocks;
@@ -538,7 +539,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
 }
 
 // The parts of a row put together, in the order of their numbers, by a wave: a lane takes D / 64 channels (D = 32: half of the lanes one
-// each).  row: the first part's, the others `step` rows apart; to: the row of the output.
+// each).  row: the first part's, the others `step` rows apart; to: the row of the output.  Only parts that do not exist are passed over: a weight
+// of zero makes an infinite sum of values NaN, as it does in a row of one part.
 template <int D>
 __device__ __forceinline__ void merge_row(const float* __restrict__ o_part, const float* __restrict__ ml_part, int parts, int64_t row, int64_t step, int64_t to,
                                           int lane, void* __restrict__ o, int o_dtype) {
@@ -555,8 +557,8 @@ __device__ __forceinline__ void merge_row(const float* __restrict__ o_part, cons
   const float den = across_lanes<0x3f>(w * l, [](float x, float y) { return x + y; });
   float x[E] = {};
   for (int s = 0; s < parts; ++s) {
+    if (__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(l), s)) == kNoPart) continue;
     const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
-    if (f == 0.f) continue;
     const float* p = &o_part[(row + s * step) * D + E * (lane & (D / E - 1))];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = fmaf(p[e], f, x[e]);
