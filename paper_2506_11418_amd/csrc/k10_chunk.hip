@@ -173,18 +173,24 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
   if (a.n_b <= 64) {
     if (!in_order(a, t_shift, wave, lane, split > 0, s_order, slot, used, mine)) return;
   } else {
-    // Sequence b has the places from (starts[b] >> t_shift) + b on: as many as it needs, or one more.
+    // Sequence b has the places from (starts[b] >> t_shift) + min(starts[b], b) on.  With c tokens, c > 0, the first term grows by c >> t_shift at
+    // least and the second by one: as many as it needs, or one more; one without tokens has none, or one.  Together no more than n tokens
+    // of as many sequences need, whatever the number of those without any.  us for tables of 4 / 65 / 256 / 4096 rows, three of which have a
+    // new token after 32768: 96 / 96 / 98 / 103 (a place for every row, which then fill the chip without parts: 94 / 226 / 631 / 923).
     if (split) slot = a.slots - 1 - slot;
     if (tid == 0) s_seq = 0;
     __syncthreads();
     int before = 0;
-    for (int i = tid; i < a.n_b; i += kThreads) before += (min(max(a.starts[i], 0), a.n) >> t_shift) + i <= slot;
+    for (int i = tid; i < a.n_b; i += kThreads) {
+      const int s = min(max(a.starts[i], 0), a.n);
+      before += (s >> t_shift) + min(s, i) <= slot;
+    }
     if (before) atomicAdd(&s_seq, before);
     __syncthreads();
     const int b = s_seq - 1;
     if (b < 0) return;
     const int first = min(max(a.starts[b], 0), a.n), last = min(max(a.starts[b + 1], 0), a.n);
-    if (!rows_of(a, t_shift, b, slot - (first >> t_shift) - b, first, last, a.lens[b], mine)) return;
+    if (!rows_of(a, t_shift, b, slot - (first >> t_shift) - min(first, b), first, last, a.lens[b], mine)) return;
   }
   const int b = mine.b, tok0 = mine.tok0, tokens = mine.tokens, len = mine.len, pos0 = mine.pos0, seen = mine.seen;
   const int rows = tokens << a.g_shift;
@@ -627,7 +633,7 @@ int64_t tail_places(int heads) { return up(groups_at_once() * (int64_t)kTailEigh
 // 9 x 700 tokens over 1500 states 56, not 40.
 ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
   ChunkCut cut;
-  cut.slots = n / (kRows / (q_heads / heads)) + (n_b <= 64 && n < n_b ? (int)most(n, 1) : n_b);
+  cut.slots = n / (kRows / (q_heads / heads)) + (int)least(most(n, 1), n_b);   // (no more sequences than tokens have any)
   const int64_t groups = (int64_t)cut.slots * heads;
   if (groups >= (int64_t)kRounds * groups_at_once()) {
     cut.span = (int)(up(most(up(max_len, kTailSplits), kSpan), 64) * 64);
