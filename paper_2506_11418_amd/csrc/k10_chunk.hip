@@ -127,13 +127,13 @@ struct Tile {
 };
 
 // 16 bytes a lane from memory into LDS, lane l's at lds + 16 l (lds: the same in all lanes).  As a builtin every later read of LDS
-// would wait for it; here the wait is the one before the tile's barrier.
+// would wait for it; here the wait is the one before the tile's barrier.  (The load has read m0 when it is issued; what the compiler had there is gone.)
 __device__ __forceinline__ void to_lds16(const void* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "m0", "memory");
 }
 // the same from a base that all lanes share
 __device__ __forceinline__ void to_lds16(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
