@@ -407,14 +407,14 @@ int ckv_paged_sparse_decode_attn(const void* q, int32_t q_heads, const void* K_p
  *            place would be before the first token sees none).  0: every one sees all lens[b] tokens (cross attention to
  *            states of another length).
  *   scale <= 0 selects 1/sqrt(dim); CKV_EUNSUPPORTED outside 1e-30 .. 1e30.
- *   o        [n, q_heads, dim] contiguous in o_dtype, 16-byte aligned: zero for a token that sees none; NaN where a logit
- *            that it sees is NaN or +inf.  Tokens that it does not see (behind it, of degree 0 or below, with a table entry
+ *   o        [n, q_heads, dim] contiguous in o_dtype, 16-byte aligned: zero for a token that sees none, or no logit above -inf; NaN where a
+ *            logit that it sees is NaN or +inf.  Tokens that it does not see (behind it, of degree 0 or below, with a table entry
  *            outside the pool) do not reach it, whatever their keys and values hold.
  *   workspace: scratch, whatever it holds (NULL where the size is 0); the size for an n and a max_len serves every smaller
  *            one and every batch.  Calls that share one must not overlap in time.
  * bf16: products on bf16 matrix instructions with fp32 sums, softmax weights rounded to bf16 (by 2^-8 at most) for the product with
  * the values; the result depends on nothing but the arguments and the number of CUs (no atomics on numbers).  fp32: fp32 throughout.
- * Infinite values that a token sees leave it an infinity or NaN.
+ * Infinite values that a token sees leave it an infinity or NaN, NaN values NaN, however small their weight.
  * Supported: q_heads / heads in {1,2,4,8}; bf16 dim 64/128; fp32 dim 32/64/128; pools of fewer than 2^31 token rows;
  * n <= 2^30; sequences (max_len, or what the table holds) of up to 2^31 - 1025 tokens. */
 int ckv_paged_chunk_attn_workspace(const ckv_paged_layout* pl, int32_t q_heads, int32_t n, int32_t max_len, size_t* bytes);

@@ -13,11 +13,11 @@
 // chain that makes S: three bf16 parts of it by ones.
 //
 // What bounds it: many new tokens, the matrix cores and the exponentials beside them: a prompt of 16384 tokens (32 heads over 8, dim 128)
-// 2050 us, 1070 TFLOP/s of the 1216 that a plain product of 8192 cubed reaches here; four turns over 16384 950.  Few, memory: 16 requests of 1
-// to 8 tokens over 32768 310 us, 5.2 TB/s, what a copy reaches.
-// Against it measured: 256 rows in eight waves, one workgroup a CU: 1068 TFLOP/s for the prompt, 850 (885) for the turns; 64 rows a wave: 740
-// to 794 (the sums no longer fit beside the rest); the next tile's S between this one's products with V 1010 to 1030; two
-// halves of a workgroup in turn 1036; waves of their own for few rows 380 us (311).
+// 2070 us, 1062 TFLOP/s, where the library's product of 8192 cubed reaches 1370 to 1605 here (by the order of its right operand); four turns
+// over 16384 970 to 985.  Few, memory: 16 requests of 1 to 8 tokens over 32768 298 us, 5.4 TB/s, what a copy reaches.
+// Measured against an earlier step, whose figure is in brackets: 256 rows in eight waves, one workgroup a CU: 1068 TFLOP/s for the prompt
+// (1070), 850 for the turns (885); 64 rows a wave: 740 to 794 (the sums no longer fit beside the rest); the next tile's S between this
+// one's products with V 1010 to 1030; two halves of a workgroup in turn 1036; waves of their own for few rows 380 us (311).
 #include <type_traits>
 
 #include "ckv_internal.h"
@@ -436,7 +436,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn_kernel(ChunkArgs a) {
       const float base = ref == -INFINITY ? 0.f : ref;   // (a row that has seen nothing yet: all weights zero)
       if constexpr (L::BF16) {
         // Weights are rounded to bf16 for the product: 2^-8 of each at most, and their sum is taken of the rounded ones, so that they
-        // still add up to one.
+        // still add up to one.  An output's error against 64 bits is 0.0021 of it (root of the mean square), 0.0016 by a bf16 output's own rounding.  The rest
+        // of each as a second bf16 part, and a second product: a prompt of 16384 2095 -> 2913 us, four turns over 16384 1416 -> 1914, drafted
+        // tokens over 32768 299 -> 321.
         const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
@@ -629,7 +631,7 @@ int64_t tail_places(int heads) { return up(groups_at_once() * (int64_t)kTailEigh
 // Places enough for kRounds rounds: the last half of a round (kTailEighths) in up to kTailSplits parts, of kSpan tokens or more (of 512 or more,
 // 64 turns of 100 over 1000 took 176 us, not 154, and 8 of 1000 over 2000 274, not 252).  Four turns of 1024 to 2048 tokens over
 // 16384 are three rounds and a little: 1537 us with whole places, 1434 so, 1428 with 8 parts, 1440 with a quarter of a round, 1446 with
-// a whole one; a prompt of 16384 tokens stays at 2050.  From one round on (kRounds 1): 39 single tokens beside 1999 975, not 908,
+// a whole one; a prompt of 16384 tokens stays as it is.  From one round on (kRounds 1): 39 single tokens beside 1999 975, not 908,
 // 9 x 700 tokens over 1500 states 56, not 40.
 ChunkCut chunk_cut(int n_b, int heads, int q_heads, int n, int max_len) {
   ChunkCut cut;

@@ -2,7 +2,7 @@
 // k8_tables.hip for its layout), and the pages of every pool that shares them are then copied by the list of pairs.
 //
 // Tables and lists are small: what their kernels take is launches and waits for loads that depend on each other (3.5 to 6.5 us each, of the
-// 12.1 us of a prompt of 500 tokens forked, copied and dropped again).  The copy is bound by memory.
+// 12 to 13.5 us of a prompt of 500 tokens forked, copied and dropped again).  The copy is bound by memory.
 #include "ckv_internal.h"
 #include "ckv_device.h"
 
@@ -478,8 +478,8 @@ hipError_t launch_paged_fork(int32_t* table, int32_t* lens, const int32_t* sourc
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ScopedTimer t("fork_deal", st);
-  // (One workgroup waits for no other: two rows, of which one continues the other, with their copy and trim 12.6 us against 13.8; rows that
-  // follow each other in it cost 1 us each: eight 22.5 against 16.4.)
+  // (One workgroup waits for no other: two rows, of which one continues the other, with their copy and trim 12.0 us against 12.6, both in
+  // turn in one process, replayed by a graph 11.6 against 13.3; rows that follow each other in it cost 1 us each: eight 22.5 against 16.4.)
   const dim3 grid(n_b <= 2 ? 1u : (unsigned)(n_b < 256 ? n_b : 256));
   if (n_b <= kThreads)
     hipLaunchKernelGGL(fork_deal_kernel<1>, grid, dim3(kThreads), (size_t)n_b * 8, st, table, lens, source, free_list, n_b, max_blocks, n_blocks, shift,
